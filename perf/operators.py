@@ -195,7 +195,7 @@ def _own_norm(s):
     if not s["case"]["train"]:
         return out
     if s["work"] is None:       # a program keeps its workspace
-        s["work"] = ctx.rtoss_block_norm_workspace(s["y"], tokens_per_gate=s["S"], gated=s["gate"] is not None)
+        s["work"] = ctx.rtoss_block_norm_workspace(s["y"], gated=s["gate"] is not None)
     ctx.rtoss_block_norm_backward(s["r"], s["y"], s["dz"], s["dn"], s["dr"], s["dy"], post=post, pre=pre, post_weight=s["wpost"],
                                   pre_weight=s["wpre"], gate=s["gate"], tokens_per_gate=s["S"], residual_scale=s["scale"], eps=EPS,
                                   dpost_weight=s["dwpost"], dpre_weight=s["dwpre"], dgate=s["dgate"], workspace=s["work"])
