@@ -516,6 +516,124 @@ rtoss_status rtoss_pool_pyramid(void* y_dev, int N, int C, int H, int W, int k, 
 rtoss_status rtoss_add_act(const void* a_dev, const void* b_dev, void* y_dev, int64_t n_elements, rtoss_dtype dtype,
                            rtoss_act act, void* cuda_stream);
 
+/* ---- operators over tokens: blocks of transformers next to the convolutions -------------------------------- */
+/* Not part of the paper's method.  A token is a row of a matrix: a position of a sequence, or a position of a
+ * channels-last map (an NHWC tensor of N x H x W positions is a matrix of N*H*W tokens, and a 1x1 convolution over it a
+ * matrix product).  Matrices are given by their first element and the distance of their rows, so they may be column
+ * slices of wider ones; what lies behind a row's last value, and rows behind the last token, are neither read nor
+ * written.  Unless a call says otherwise, operands must not overlap outputs.  No call keeps memory or anything else
+ * from one call to the next: workspaces are the caller's, calls may be captured into CUDA graphs, and several threads
+ * may call on one context, each on a stream of its own (with workspaces of its own).  tokens = 0 is valid: nothing is
+ * launched, except that the gradients of weights are set to zero.  Device-side waits are bounded and report through
+ * rtoss_device_status like those of the convolutions. */
+typedef struct {
+    void* dev;          /* first element */
+    int64_t row_stride; /* elements from one row to the next, 0 = rows follow one another */
+} rtoss_rows;
+
+/* Rows to 8-bit integers with one scale each: scale[r] = max_c |x[r,c]| / 127, q[r,c] = x[r,c] / scale[r] rounded to the
+ * nearest integer, halves to even (both quotients in fp32).  A row of zeros has scale 0 and codes 0; a row that holds
+ * an infinity or a NaN has scale NaN and codes 0, so that whatever is made from it is NaN.  For activations (a scale
+ * for each token) and for weights alike (a scale for each output channel: [Cout][Cin] rows, for instance those of
+ * rtoss_packed_to_dense for a pruned 1x1 layer).  x: fp32, bf16 or fp16, any row strides; rtoss_matmul_i8 asks for rows
+ * of q that start on 16-byte boundaries.  Errors: RTOSS_ERR_INVALID_ARG, RTOSS_ERR_CUDA. */
+rtoss_status rtoss_quantize_rows(rtoss_ctx* ctx, const void* x_dev, rtoss_dtype dtype, int64_t rows, int cols, int64_t x_row_stride,
+                                 int8_t* q_dev, int64_t q_row_stride, float* scale_dev, void* cuda_stream);
+
+/* Matrix product in 8-bit integers with a scale for each token and each output channel:
+ *   y[t,n] = act( x_scale[t] * w_scale[n] * sum_k x[t,k] * w[n,k] + bias[n] + residual[t,n] )
+ * with residual_after_act the residual is added behind the activation instead.  The sum is an exact 32-bit integer (any
+ * codes, -128 included); scales, bias, activation and residual are applied in fp32 and rounded once to y_dtype.
+ * residual (dev NULL: none) has y's type and may be y itself.  At most sixteen tokens run on kernels that read each
+ * weight once straight into registers; more on the tensor cores (tcgen05, CTA pairs).
+ * Rows of x, w, y and the residual start on 16-byte boundaries (base and row stride; tokens, K and N may be any), scales
+ * and bias are 16-byte aligned: else RTOSS_ERR_ALIGNMENT.  K above 131071 (where a sum could leave 32 bits):
+ * RTOSS_ERR_UNSUPPORTED. */
+typedef struct {
+    int64_t tokens;
+    int K, N;
+    rtoss_rows x;  /* int8 [tokens][K] */
+    rtoss_rows w;  /* int8 [N][K] */
+    rtoss_rows y;  /* y_dtype [tokens][N] */
+    rtoss_rows residual;
+    const float* x_scale_dev; /* [tokens] */
+    const float* w_scale_dev; /* [N] */
+    const float* bias_dev;    /* [N] or NULL */
+    rtoss_dtype y_dtype;
+    rtoss_act act;
+    int residual_after_act;
+} rtoss_i8_product;
+rtoss_status rtoss_matmul_i8(rtoss_ctx* ctx, const rtoss_i8_product* product, void* cuda_stream);
+
+/* A gated feed-forward block over tokens (bf16 or fp16; fp32 sums):
+ *   g = x Wg^T,  u = x Wu^T,  h = act(g) * u,  y = h Wd^T
+ * Forward: both projections, the activation and the product are one kernel, the product with Wd a second one; w_down and
+ * y may be NULL together (h is the result then).  gate and up, if given, receive g and u, which the backward pass needs.
+ * h is written either way.
+ * Backward, from x, the weights, gate, up and dy:
+ *   dh = dy Wd,  dgate = dh * u * act'(g),  dup = dh * act(g)   (h is formed again on the way; act' of ReLU at 0 is 0)
+ *   dx = dgate Wg + dup Wu,  dw_gate = dgate^T x,  dw_up = dup^T x,  dw_down = dy^T h
+ * in three launches.  dx, dw_gate, dw_up, dw_down are each left out when NULL (x, w_gate and w_up may be NULL where no
+ * gradient that is asked for needs them).  dgate may be gate itself and dup up (their contents are then spent).
+ * Intermediate values pass through memory in the data type.  The order of every sum is fixed: same inputs, same bits.
+ * All rows start on 16-byte boundaries, else RTOSS_ERR_ALIGNMENT (tokens, D and F may be any).  fp32 data:
+ * RTOSS_ERR_UNSUPPORTED. */
+typedef struct {
+    int64_t tokens;
+    int D, F;
+    rtoss_dtype dtype;
+    rtoss_act act;
+    rtoss_rows x;               /* [tokens][D] */
+    rtoss_rows w_gate, w_up;    /* [F][D] */
+    rtoss_rows w_down;          /* [D][F] */
+    rtoss_rows h;               /* [tokens][F], output (workspace) of both calls */
+    rtoss_rows gate, up;        /* [tokens][F] */
+    rtoss_rows y;               /* [tokens][D], forward */
+    rtoss_rows dy;              /* [tokens][D], from here on backward only */
+    rtoss_rows dgate, dup;      /* [tokens][F], outputs (workspace) */
+    rtoss_rows dx;              /* [tokens][D] */
+    rtoss_rows dw_gate, dw_up;  /* [F][D] */
+    rtoss_rows dw_down;         /* [D][F] */
+} rtoss_ffn;
+rtoss_status rtoss_gated_ffn_forward(rtoss_ctx* ctx, const rtoss_ffn* ffn, void* cuda_stream);
+rtoss_status rtoss_gated_ffn_backward(rtoss_ctx* ctx, const rtoss_ffn* ffn, void* cuda_stream);
+
+/* The norm behind one block and the norm in front of the next, with the block's gate and the residual between them:
+ *   v = norm_post(y),  z = residual_scale * r + gate * v,  n = norm_pre(z)
+ * r: the residual stream, y: the block's output.  RTOSS_NORM_RMS: t / sqrt(mean(t^2) + eps) * weight; RTOSS_NORM_LAYER: the
+ * same with t's mean subtracted first; RTOSS_NORM_NONE: v = y resp. no n.  Weights are fp32 [D] (NULL: ones).  The gate
+ * (dev NULL: none) has one row of D values in the data type for every tokens_per_gate consecutive tokens (tokens: one
+ * learned gate for all; fewer: one per sample); it must divide the tokens.  n is taken from z before z is rounded.
+ * fp32, bf16 or fp16 data, any strides and alignment (rows on 16-byte boundaries with D a multiple of 8 are faster);
+ * fp32 arithmetic, rounded once.  z may be r or y itself, and so may n (not the same one as z).
+ * Backward, from r, y and the gradients dz and dn of z and n (each may be NULL = zero): dr, dy and, where not NULL,
+ * dpost_weight, dpre_weight (fp32 [D]) and dgate (like gate, summed over the tokens that share it).  v and z are formed
+ * again from r and y, so neither may have been overwritten.  dr and dy may be dz and dn themselves.  The sums over
+ * tokens need workspace_dev (16-byte aligned, rtoss_block_norm_workspace floats, nothing kept in it between calls);
+ * their order is fixed by the sizes and the device: same inputs, same bits. */
+typedef enum { RTOSS_NORM_NONE = 0, RTOSS_NORM_RMS = 1, RTOSS_NORM_LAYER = 2 } rtoss_norm;
+typedef struct {
+    int64_t tokens;
+    int D;
+    rtoss_dtype dtype;
+    rtoss_norm post, pre;
+    float residual_scale, eps;
+    int64_t tokens_per_gate;
+    const float* post_weight_dev;
+    const float* pre_weight_dev;
+    rtoss_rows r, y, gate;
+    rtoss_rows z, n;                         /* forward */
+    rtoss_rows dz, dn, dr, dy, dgate;        /* from here on backward only */
+    float* dpost_weight_dev;
+    float* dpre_weight_dev;
+    float* workspace_dev;
+    int64_t workspace_floats;
+} rtoss_block_norm;
+rtoss_status rtoss_block_norm_forward(rtoss_ctx* ctx, const rtoss_block_norm* norm, void* cuda_stream);
+rtoss_status rtoss_block_norm_backward(rtoss_ctx* ctx, const rtoss_block_norm* norm, void* cuda_stream);
+/* Floats that a backward call of this size needs as workspace (host arithmetic; gated: a dgate is asked for). */
+rtoss_status rtoss_block_norm_workspace(const rtoss_ctx* ctx, int64_t tokens, int D, int gated, int64_t* floats);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,6 +7,7 @@ used for device memory and streams only).
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -14,6 +15,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "librtoss.so")
 
 OK = 0
+ERR_INVALID_ARG = 1
 ERR_UNSUPPORTED = 3
 F32, BF16, F16 = 0, 1, 2
 NCHW, NHWC = 0, 1
@@ -24,6 +26,8 @@ POOL_PYRAMID_PX = 6400
 ROUTE_TENSOR, ROUTE_TENSOR_REPACKED, ROUTE_STEM, ROUTE_FEW, ROUTE_STAGED = 0, 1, 2, 3, 4
 DTYPE_NAMES = {"f32": F32, "bf16": BF16, "f16": F16}
 ACT_NAMES = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU}
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+NORM_NAMES = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
 
 SYMBOLS = [
     "rtoss_create", "rtoss_destroy", "rtoss_status_string", "rtoss_last_error", "rtoss_pattern_preset",
@@ -35,7 +39,15 @@ SYMBOLS = [
     "rtoss_batch_create", "rtoss_batch_select_pack", "rtoss_batch_destroy",
     "rtoss_select_patterns_shared", "rtoss_conv_group", "rtoss_set_wait_limit", "rtoss_inject_lost_copy",
     "rtoss_fma_plan3x3", "rtoss_conv_chain", "rtoss_chain_deps", "rtoss_chain_deps_spans", "rtoss_tensor_plan_of",
+    "rtoss_quantize_rows", "rtoss_matmul_i8", "rtoss_gated_ffn_forward", "rtoss_gated_ffn_backward",
+    "rtoss_block_norm_forward", "rtoss_block_norm_backward", "rtoss_block_norm_workspace",
 ]
+
+# The argument structs of the operators over tokens (rtoss_i8_product, rtoss_ffn, rtoss_block_norm), packed field by field:
+# "Qq" is a matrix (rtoss_rows).  (A ctypes structure of this many fields takes longer to fill than a small call to run.)
+_I8_PRODUCT = struct.Struct("@q2i" + "Qq" * 4 + "3Q3i4x")
+_FFN = struct.Struct("@q4i" + "Qq" * 15)
+_BLOCK_NORM = struct.Struct("@q4i2fq2Q" + "Qq" * 10 + "3Qq")
 
 
 class RtossError(RuntimeError):
@@ -132,6 +144,13 @@ def _load():
     lib.rtoss_upsample2x_slice.argtypes = [vp, ci, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp]
     lib.rtoss_pool_pyramid.argtypes = [vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, vp]
     lib.rtoss_add_act.argtypes = [vp, vp, vp, ctypes.c_int64, ci, ci, vp]
+    lib.rtoss_quantize_rows.argtypes = [vp, vp, ci, ctypes.c_int64, ci, ctypes.c_int64, vp, ctypes.c_int64, vp, vp]
+    lib.rtoss_matmul_i8.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.rtoss_gated_ffn_forward.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.rtoss_gated_ffn_backward.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.rtoss_block_norm_forward.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.rtoss_block_norm_backward.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.rtoss_block_norm_workspace.argtypes = [vp, ctypes.c_int64, ci, ci, ctypes.POINTER(ctypes.c_int64)]
     lib.rtoss_pattern_usage.argtypes = [vp, vp, ci, ctypes.c_int64, vp, ci, ci, vp, vp, vp]
     lib.rtoss_batch_create.argtypes = [vp, ctypes.POINTER(BatchItem), ci, ctypes.POINTER(vp)]
     lib.rtoss_batch_select_pack.argtypes = [vp, vp, vp]
@@ -340,6 +359,50 @@ def _first_stream():
     return s.cuda_stream
 
 
+def _stream_on(device):
+    """The current stream of the given device."""
+    if _raw_stream is not None:
+        return _raw_stream(device)
+    _first_stream()
+    if _raw_stream is not None:
+        return _raw_stream(device)
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _bad(what, why):
+    raise RtossError(ERR_INVALID_ARG, "%s: %s" % (what, why))
+
+
+def _matrix(t, rows, cols, dtype, device, what):
+    """(address, row stride) of a CUDA matrix [rows, cols] whose values of a row are neighbours; (0, 0) for None."""
+    if t is None:
+        return 0, 0
+    if t.dtype is not dtype or t.dim() != 2 or t.size(0) != rows or t.size(1) != cols:
+        _bad(what, "need %s [%d, %d], got %s %s" % (dtype, rows, cols, t.dtype, list(t.shape)))
+    if t.get_device() != device:
+        _bad(what, "is not on the context's device")
+    step, inner = t.stride()
+    if inner != 1 and cols > 1:
+        _bad(what, "the values of a row must be neighbours in memory")
+    if rows <= 1:
+        step = (cols + 15) // 16 * 16     # (no second row)
+    elif step < cols:
+        _bad(what, "rows overlap")
+    return t.data_ptr(), step
+
+
+def _vector(t, n, dtype, device, what):
+    """Address of a contiguous CUDA vector [n]; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
+        _bad(what, "need contiguous %s [%d], got %s %s" % (dtype, n, t.dtype, list(t.shape)))
+    if t.get_device() != device:
+        _bad(what, "is not on the context's device")
+    return t.data_ptr()
+
+
 class Context:
     """Owns an rtoss_ctx on one CUDA device."""
 
@@ -506,6 +569,110 @@ class Context:
                        y_channel_stride, path)
         self._check(lib.rtoss_conv_pattern_host(self.h, packed.h, x_host.data_ptr(), y_host.data_ptr(), ctypes.byref(d)))
         return y_host
+
+    # -- operators over tokens (matrices are 2-D CUDA tensors; column slices are fine) ------------------------------------
+    def rtoss_quantize_rows(self, x, q, scale):
+        """x [rows, cols] fp32 / bf16 / fp16 -> int8 codes q [rows, cols] and fp32 scale [rows]."""
+        import torch
+        rows, cols = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
+        xp, xs = _matrix(x, rows, cols, x.dtype, self.device, "x")
+        qp, qs = _matrix(q, rows, cols, torch.int8, self.device, "q")
+        st = lib.rtoss_quantize_rows(self.h, xp, _torch_dtype_code(x), rows, cols, xs, qp, qs,
+                                     _vector(scale, rows, torch.float32, self.device, "scale"), _stream_on(self.device))
+        if st:
+            self._check(st)
+        return q, scale
+
+    def rtoss_matmul_i8(self, x, x_scale, w, w_scale, y, act=ACT_NONE, bias=None, residual=None, residual_after_act=False):
+        """y [tokens, N] = act(x_scale * w_scale * (x [tokens, K] @ w [N, K]^T) + bias + residual)."""
+        import torch
+        tokens, K = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
+        N, d, f32 = w.size(0), self.device, torch.float32
+        st = lib.rtoss_matmul_i8(self.h, _I8_PRODUCT.pack(
+            tokens, K, N, *_matrix(x, tokens, K, torch.int8, d, "x"), *_matrix(w, N, K, torch.int8, d, "w"),
+            *_matrix(y, tokens, N, y.dtype, d, "y"), *_matrix(residual, tokens, N, y.dtype, d, "residual"),
+            _vector(x_scale, tokens, f32, d, "x_scale"), _vector(w_scale, N, f32, d, "w_scale"), _vector(bias, N, f32, d, "bias"),
+            _torch_dtype_code(y), act, 1 if residual_after_act else 0), _stream_on(d))
+        if st:
+            self._check(st)
+        return y
+
+    def rtoss_gated_ffn_forward(self, x, w_gate, w_up, w_down, h, y, gate=None, up=None, act=ACT_SILU):
+        """h [tokens, F] = act(x w_gate^T) * (x w_up^T), y [tokens, D] = h w_down^T; gate, up: kept for the backward pass.
+        w_down and y may be None together.  Returns y, or h."""
+        tokens, D = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
+        F, t, d = w_gate.size(0), x.dtype, self.device
+        st = lib.rtoss_gated_ffn_forward(self.h, _FFN.pack(
+            tokens, D, F, _torch_dtype_code(x), act, *_matrix(x, tokens, D, t, d, "x"), *_matrix(w_gate, F, D, t, d, "w_gate"),
+            *_matrix(w_up, F, D, t, d, "w_up"), *_matrix(w_down, D, F, t, d, "w_down"), *_matrix(h, tokens, F, t, d, "h"),
+            *_matrix(gate, tokens, F, t, d, "gate"), *_matrix(up, tokens, F, t, d, "up"), *_matrix(y, tokens, D, t, d, "y"),
+            0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
+        if st:
+            self._check(st)
+        return h if y is None else y
+
+    def rtoss_gated_ffn_backward(self, x, w_gate, w_up, w_down, gate, up, dy, h, dgate, dup, dx=None, dw_gate=None, dw_up=None,
+                                 dw_down=None, act=ACT_SILU):
+        """Gradients of rtoss_gated_ffn_forward from dy and the kept gate and up, into those of dx, dw_gate, dw_up, dw_down
+        that are given; h, dgate, dup [tokens, F] are workspaces (dgate may be gate and dup up)."""
+        tokens, D = dy.shape if dy.dim() == 2 else _bad("dy", "need a matrix")
+        F, t, d = w_down.size(1) if w_down.dim() == 2 else _bad("w_down", "need a matrix"), dy.dtype, self.device
+        st = lib.rtoss_gated_ffn_backward(self.h, _FFN.pack(
+            tokens, D, F, _torch_dtype_code(dy), act, *_matrix(x, tokens, D, t, d, "x"), *_matrix(w_gate, F, D, t, d, "w_gate"),
+            *_matrix(w_up, F, D, t, d, "w_up"), *_matrix(w_down, D, F, t, d, "w_down"), *_matrix(h, tokens, F, t, d, "h"),
+            *_matrix(gate, tokens, F, t, d, "gate"), *_matrix(up, tokens, F, t, d, "up"), 0, 0, *_matrix(dy, tokens, D, t, d, "dy"),
+            *_matrix(dgate, tokens, F, t, d, "dgate"), *_matrix(dup, tokens, F, t, d, "dup"), *_matrix(dx, tokens, D, t, d, "dx"),
+            *_matrix(dw_gate, F, D, t, d, "dw_gate"), *_matrix(dw_up, F, D, t, d, "dw_up"),
+            *_matrix(dw_down, D, F, t, d, "dw_down")), _stream_on(d))
+        if st:
+            self._check(st)
+        return dx, dw_gate, dw_up, dw_down
+
+    def rtoss_block_norm_forward(self, r, y, z, n=None, post=NORM_RMS, pre=NORM_RMS, post_weight=None, pre_weight=None, gate=None,
+                                 tokens_per_gate=0, residual_scale=1.0, eps=1e-6):
+        """z = residual_scale * r + gate * norm_post(y), n = norm_pre(z); gate [tokens / tokens_per_gate, D] (0: all tokens
+        share one).  Returns (z, n)."""
+        import torch
+        tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
+        t, d, f32 = y.dtype, self.device, torch.float32
+        share = tokens_per_gate or max(tokens, 1)
+        st = lib.rtoss_block_norm_forward(self.h, _BLOCK_NORM.pack(
+            tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, D, f32, d, "post_weight"),
+            _vector(pre_weight, D, f32, d, "pre_weight"), *_matrix(r, tokens, D, t, d, "r"), *_matrix(y, tokens, D, t, d, "y"),
+            *_matrix(gate, max(tokens // share, 1), D, t, d, "gate"), *_matrix(z, tokens, D, t, d, "z"),
+            *_matrix(n, tokens, D, t, d, "n"), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
+        if st:
+            self._check(st)
+        return z, n
+
+    def rtoss_block_norm_workspace(self, y, gated=False):
+        """A workspace for rtoss_block_norm_backward on matrices like y (gated: with a dgate)."""
+        import torch
+        n = ctypes.c_int64(0)
+        self._check(lib.rtoss_block_norm_workspace(self.h, y.size(0), y.size(1), 1 if gated else 0, ctypes.byref(n)))
+        return torch.empty(n.value, dtype=torch.float32, device=y.device)
+
+    def rtoss_block_norm_backward(self, r, y, dz, dn, dr, dy, post=NORM_RMS, pre=NORM_RMS, post_weight=None, pre_weight=None,
+                                  gate=None, tokens_per_gate=0, residual_scale=1.0, eps=1e-6, dpost_weight=None, dpre_weight=None,
+                                  dgate=None, workspace=None):
+        """Gradients dr, dy, dpost_weight, dpre_weight (fp32 [D]) and dgate of rtoss_block_norm_forward from dz and dn (either
+        may be None)."""
+        import torch
+        tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
+        t, d, f32 = y.dtype, self.device, torch.float32
+        share = tokens_per_gate or max(tokens, 1)
+        gates = max(tokens // share, 1)
+        floats = 0 if workspace is None else workspace.numel()
+        st = lib.rtoss_block_norm_backward(self.h, _BLOCK_NORM.pack(
+            tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, D, f32, d, "post_weight"),
+            _vector(pre_weight, D, f32, d, "pre_weight"), *_matrix(r, tokens, D, t, d, "r"), *_matrix(y, tokens, D, t, d, "y"),
+            *_matrix(gate, gates, D, t, d, "gate"), 0, 0, 0, 0, *_matrix(dz, tokens, D, t, d, "dz"), *_matrix(dn, tokens, D, t, d, "dn"),
+            *_matrix(dr, tokens, D, t, d, "dr"), *_matrix(dy, tokens, D, t, d, "dy"), *_matrix(dgate, gates, D, t, d, "dgate"),
+            _vector(dpost_weight, D, f32, d, "dpost_weight"), _vector(dpre_weight, D, f32, d, "dpre_weight"),
+            _vector(workspace, floats, f32, d, "workspace"), floats), _stream_on(d))
+        if st:
+            self._check(st)
+        return dr, dy
 
 
 class Batch:

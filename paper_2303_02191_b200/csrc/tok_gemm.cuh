@@ -1,0 +1,654 @@
+// Matrix products over tokens on the 5th-generation tensor cores: what the gated feed-forward block (tok_ffn.cu) and the
+// 8-bit product (tok_i8.cu) share.
+//
+//   D[m, n] = sum over k of A[m, k] * B[n, k],   fp32 (16-bit operands) or exact 32-bit integer (8-bit operands) sums
+//
+// bound: the tensor pipes once a product has a few hundred tokens, the weights' bytes below that.
+//   * A tile is 256 rows x BN columns and belongs to a pair of CTAs (cta_group::2): each holds its 128 rows of A and half of
+//     B's rows in shared memory, and the pair's leader issues instructions of 256 x BN x 32 bytes.  An SM then reads 8 KB
+//     and receives 8 KB per instruction of 128 clocks (BN = 256): with a tile of its own a CTA would need 12 and 12, more
+//     than the 128 bytes a clock that shared memory moves.
+//   * An operand lies in memory either with k along its rows ("K-major": activations, and weights as [out, in]) or with k
+//     across them (gradients of weights contract over the tokens; gradients of inputs over the output features).  Both go
+//     into shared memory in rows of 128 bytes with the 128-byte swizzle, and the instruction descriptor says which it is:
+//     nothing is transposed in memory.
+//   * Warp roles: warp 0 issues TMA copies, warp 1 of the leader issues tcgen05.mma, warp 2 owns the TMEM allocation, eight
+//     epilogue warps read the accumulators (two stages: the epilogue of a tile runs under the products of the next), round
+//     into shared memory and leave the rest to TMA stores, which also cut off what lies outside the matrix.
+//   * CTA pairs are persistent and walk the tiles of up to three products (the weight gradients of the block) in groups of
+//     eight row tiles, so that the tiles in flight share their operands in L2.
+//   * Products with few tiles are cut along k: the pairs of a cluster of 2 KS CTAs take a share of k each, and exchange their
+//     fp32 sums through distributed shared memory; the shares are added in a fixed order.
+//   * Every wait is bounded; one that runs out leaves a code in the context's status word and the CTA goes through the normal
+//     exit (TMEM is always released).
+#ifndef RTOSS_TOK_GEMM_CUH
+#define RTOSS_TOK_GEMM_CUH
+
+#include <cuda.h>
+
+#include "conv_common.cuh"
+#include "tok_math.cuh"
+
+namespace rtoss_tok {
+
+using rtoss_dev::from_f32;
+using rtoss_dev::to_f32;
+
+enum GemmMode {
+    kPlain = 0,     // D, rounded to 16 bits
+    kGated = 1,     // B holds BN/2 rows of the gate's weights and BN/2 of the up projection's: h = act(gate) * up
+    kGateGrad = 2,  // D = dh: with the saved gate and up projections, their gradients and h again
+    kInt8 = 3       // 8-bit operands: scales, bias, activation, residual
+};
+
+constexpr int kGemmThreads = 384;
+constexpr int kEpiWarps = 8;
+constexpr int kMaxKS = 4;   // shares of k: clusters of at most 8 CTAs
+
+struct GemmProblem {
+    CUtensorMap a[2], b[2], o[3];   // operands by k segment (kGated: b by half), outputs
+    void* op[3];                    // the outputs again, for columns that a TMA store cannot cut off
+    long long o_ld[3];
+    int M, N;                       // rows and columns of the output
+    int tiles_m, tiles_n, first;    // first: number of the first tile
+    int kb0, kb;                    // blocks of 128 bytes of k: of the first segment, of both
+};
+
+template <int NP>
+struct GemmArgs {
+    GemmProblem p[NP];
+    int n_problems, tiles, KS;
+    int a_mn, b_mn;                 // operand lies with k across its rows
+    unsigned idesc;
+    int act;
+    int save;                       // kGated: gate and up are written too
+    int* status;
+    long long wait;
+    // kGateGrad: the saved projections; kInt8: scales, bias, residual
+    const void* e0;
+    const void* e1;
+    long long e_ld, e1_ld;
+    const float* row_scale;
+    const float* col_scale;
+    const float* bias;
+    int res_after;
+};
+
+// ---- shapes of a kernel -------------------------------------------------------------------------------------------
+template <int MODE, int BN, typename T>
+struct GemmShape {
+    static constexpr int kABytes = 128 * 128;
+    static constexpr int kBBytes = BN / 2 * 128;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kUnitAcc = MODE == kPlain || MODE == kGated ? 64 : 32;   // accumulators a lane handles at a time
+    static constexpr int kUnitCols = MODE == kPlain ? 64 : 32;                     // output columns of such a unit
+    static constexpr int kUnits = BN / kUnitAcc;
+    static constexpr int kOutRow = kUnitCols * (int)sizeof(T);                     // bytes of a staged output row: 64 or 128
+    static constexpr int kOuts = MODE == kGated || MODE == kGateGrad ? 3 : 1;
+    static constexpr int kStagingBytes = kOutRow * 32 * kOuts;                     // of a warp
+    static constexpr int kRoom = 226 * 1024 - kEpiWarps * kStagingBytes;
+    static constexpr int kStages = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
+    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 256;
+    static constexpr int kTileN = MODE == kGated ? BN / 2 : BN;                    // output columns of a tile
+    static constexpr int kTmemCols = 2 * BN;
+    // the exchange of a split tile lies in the operand ring
+    static_assert(kUnits * 4 * 32 * kUnitAcc * 4 <= kStages * kStageBytes, "no room for the exchange");
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+    static_assert(kTmemCols <= 512, "TMEM");
+};
+
+// ---- PTX ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(unsigned bar, unsigned count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ unsigned bar_try(unsigned bar, unsigned parity) {
+    unsigned done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+__device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, long long limit) {
+    if (bar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        if (bar_try(bar, parity)) return true;
+        if (clock64() - t0 > limit) return false;
+    }
+}
+__device__ __forceinline__ unsigned cta_rank() {
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ unsigned at_rank(unsigned addr, unsigned rank) {
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned elect() {
+    unsigned e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e;
+}
+// (bar: in this CTA or in the pair's other one)
+__device__ __forceinline__ void load_box(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap* map, int x, int y, unsigned src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
+// Start address, strides and swizzle of an operand in shared memory (1024-byte aligned tiles, rows of 128 bytes).  K-major: a
+// row is one m or n, groups of eight rows 1024 bytes apart.  Otherwise a row is one k with 64 values of m or n: groups of
+// eight k are 1024 bytes apart, the next 64 values of m or n `block` bytes.
+__device__ __forceinline__ unsigned long long operand_desc(unsigned addr, bool mn, unsigned block) {
+    unsigned long long d = 0;
+    d |= (unsigned long long)((addr & 0x3FFFFu) >> 4);
+    d |= (unsigned long long)(mn ? block >> 4 : 1u) << 16;
+    d |= (unsigned long long)(1024u >> 4) << 32;
+    d |= (unsigned long long)1 << 46;
+    d |= (unsigned long long)2 << 61;
+    return d;
+}
+template <bool I8>
+__device__ __forceinline__ void mma_pair(unsigned leader, unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned add) {
+    if (I8)
+        asm volatile(
+            "{\n\t.reg .pred p, pe;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 pe, %5, 0;\n\t"
+            "@pe tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, pe;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 pe, %5, 0;\n\t"
+            "@pe tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader)
+            : "memory");
+}
+// arrives at this barrier of both CTAs of the pair when the instructions issued so far are done
+__device__ __forceinline__ void commit_pair(unsigned leader, unsigned bar, unsigned short mask) {
+    asm volatile(
+        "{\n\t.reg .pred pe;\n\tsetp.ne.b32 pe, %2, 0;\n\t"
+        "@pe tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar), "h"(mask), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(unsigned at, unsigned* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void st_shared16(unsigned at, unsigned a, unsigned b, unsigned c, unsigned d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void st_cluster16(unsigned at, unsigned a, unsigned b, unsigned c, unsigned d) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(unsigned at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// ---- rounding into the staged rows ----------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ unsigned pack_pair(float lo, float hi);
+template <> __device__ __forceinline__ unsigned pack_pair<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const unsigned*>(&v);
+}
+template <> __device__ __forceinline__ unsigned pack_pair<__half>(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const unsigned*>(&v);
+}
+template <typename T> __device__ __forceinline__ float2 unpack_pair(unsigned v);
+template <> __device__ __forceinline__ float2 unpack_pair<__nv_bfloat16>(unsigned v) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&v)); }
+template <> __device__ __forceinline__ float2 unpack_pair<__half>(unsigned v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
+
+// COLS values of a lane's row into its place in the warp's staging patch, in 16-byte pieces where the TMA store with the
+// 128-byte (64-byte) swizzle looks for them; the lanes of a piece hit different banks.
+template <typename T, int COLS>
+__device__ __forceinline__ void stage_row(unsigned patch, int lane, const float* v) {
+    constexpr int kRow = COLS * (int)sizeof(T);
+    static_assert(kRow == 128 || kRow == 64, "rows of a swizzle span");
+    const unsigned row = patch + (unsigned)(lane * kRow), x = kRow == 128 ? (unsigned)(lane & 7) : (unsigned)((lane >> 1) & 3);
+    constexpr int kPer = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int j = 0; j < kRow / 16; ++j) {
+        const float* e = v + j * kPer;
+        const unsigned at = row + (((unsigned)j ^ x) << 4);
+        if constexpr (sizeof(T) == 4) st_shared16(at, __float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3]));
+        else st_shared16(at, pack_pair<T>(e[0], e[1]), pack_pair<T>(e[2], e[3]), pack_pair<T>(e[4], e[5]), pack_pair<T>(e[6], e[7]));
+    }
+}
+
+// One 16-byte piece of a 64-byte row of 16-bit values.
+template <typename T>
+__device__ __forceinline__ void stage_piece(unsigned patch, int lane, int j, const float* e) {
+    st_shared16(patch + (unsigned)(lane * 64) + (((unsigned)j ^ (unsigned)((lane >> 1) & 3)) << 4), pack_pair<T>(e[0], e[1]), pack_pair<T>(e[2], e[3]),
+                pack_pair<T>(e[4], e[5]), pack_pair<T>(e[6], e[7]));
+}
+
+// A lane's staged row to the first `cols` columns of its place in the matrix: a TMA store cuts rows off in steps of 16 bytes only.
+template <typename T, int COLS>
+__device__ __forceinline__ void unstage_row(unsigned patch, int lane, void* base, long long ld, int row, int rows, int col, int cols) {
+    constexpr int kRow = COLS * (int)sizeof(T), kPer = 16 / (int)sizeof(T);
+    if (row >= rows) return;
+    const unsigned x = kRow == 128 ? (unsigned)(lane & 7) : (unsigned)((lane >> 1) & 3);
+    T* at = reinterpret_cast<T*>(base) + (long long)row * ld + col;
+    for (int j = 0; j * kPer < cols - col; ++j) {
+        const uint4 v = ld_shared16(patch + (unsigned)(lane * kRow) + (((unsigned)j ^ x) << 4));
+        const T* e = reinterpret_cast<const T*>(&v);
+        if (cols - col >= (j + 1) * kPer) {
+            *reinterpret_cast<uint4*>(at + j * kPer) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (col + j * kPer + i < cols) at[j * kPer + i] = e[i];
+        }
+    }
+}
+
+// 32 consecutive values of one row of a [rows, cols] operand of the epilogue (zeros outside; no byte behind the row's last
+// value is read).
+template <typename T>
+__device__ __forceinline__ void fetch32(const void* base, long long ld, int row, int rows, int col, int cols, uint4* e) {
+    constexpr int kPer = 16 / (int)sizeof(T);
+    const T* at = reinterpret_cast<const T*>(base) + (long long)row * ld + col;
+#pragma unroll
+    for (int j = 0; j < 32 / kPer; ++j) {
+        e[j] = make_uint4(0u, 0u, 0u, 0u);
+        const int c = col + j * kPer;
+        if (row < rows && c < cols) {
+            if (c + kPer <= cols) {
+                e[j] = *reinterpret_cast<const uint4*>(at + j * kPer);
+            } else {
+                T part[kPer];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) part[i] = c + i < cols ? at[j * kPer + i] : from_f32<T>(0.f);
+                e[j] = *reinterpret_cast<const uint4*>(part);
+            }
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ float value_of(const uint4* e, int j) {
+    const unsigned* w = reinterpret_cast<const unsigned*>(e);
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+    else {
+        const float2 p = unpack_pair<T>(w[j >> 1]);
+        return j & 1 ? p.y : p.x;
+    }
+}
+
+// ---- the kernel -----------------------------------------------------------------------------------------------------
+template <typename T, int MODE, int BN, int NP>
+__global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_constant__ GemmArgs<NP> g) {
+    using S = GemmShape<MODE, BN, T>;
+    extern __shared__ unsigned char smem_raw[];
+    const unsigned raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    const unsigned s_stage = base, s_out = base + S::kStages * S::kStageBytes, s_bar = s_out + kEpiWarps * S::kStagingBytes;
+    const unsigned b_full = s_bar, b_empty = s_bar + 64, b_acc_full = s_bar + 128, b_acc_empty = s_bar + 144, s_tmem = s_bar + 160;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const unsigned rank = cta_rank(), half = rank & 1u, lead_rank = rank & ~1u, share = rank >> 1;
+    const int KS = g.KS;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (warp == 0 && lane < 7) {
+        const GemmProblem& p = g.p[0];
+        const CUtensorMap* m = lane < 2 ? &p.a[lane] : lane < 4 ? &p.b[lane - 2] : &p.o[lane - 4];
+        asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+    }
+    if (warp == 1 && lane == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            bar_init(b_full + 8 * i, 1);
+            bar_init(b_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(b_acc_full + 8 * i, 1);
+            bar_init(b_acc_empty + 8 * i, 2 * kEpiWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_tmem), "r"(S::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_barrier();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    unsigned tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(s_tmem));
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    const int cluster = (int)blockIdx.x / (2 * KS), clusters = (int)gridDim.x / (2 * KS);
+    struct Tile {
+        const GemmProblem* p;
+        int mt, nt;
+    };
+    auto tile_of = [&](int t) {
+        int i = 0;
+        if (NP > 1)
+            while (i + 1 < g.n_problems && t >= g.p[i + 1].first) ++i;
+        const GemmProblem& p = g.p[i];
+        const int lt = t - p.first, per = 8 * p.tiles_n, grp = lt / per, r = lt - grp * per, gm = min(8, p.tiles_m - 8 * grp);
+        Tile at;
+        at.p = &p;
+        at.nt = r / gm;
+        at.mt = 8 * grp + (r - at.nt * gm);
+        return at;
+    };
+    // this pair's blocks of k
+    auto kb_begin = [&](const GemmProblem& p) { return (int)((long long)p.kb * share / KS); };
+    auto kb_end = [&](const GemmProblem& p) { return (int)((long long)p.kb * (share + 1) / KS); };
+    constexpr int kPerBlock = MODE == kInt8 ? 128 : 64;   // values of k in 128 bytes
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            unsigned ph = 0;
+            bool ok = true;
+            for (int t = cluster; t < g.tiles && ok; t += clusters) {
+                const Tile at = tile_of(t);
+                const GemmProblem& p = *at.p;
+                const int m0 = at.mt * 256 + (int)half * 128;
+                const int n0 = MODE == kGated ? at.nt * (BN / 2) : at.nt * BN + (int)half * (BN / 2);
+                for (int kb = kb_begin(p), e = kb_end(p); kb < e; ++kb) {
+                    if (!(ok = bar_wait(b_empty + 8 * s, ph ^ 1u, g.wait))) break;
+                    const unsigned sa = s_stage + (unsigned)(s * S::kStageBytes), sb = sa + S::kABytes;
+                    if (half == 0)
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b_full + 8 * s), "r"(2 * S::kStageBytes) : "memory");
+                    const unsigned bar = at_rank(b_full + 8 * s, lead_rank);
+                    const int seg = kb >= p.kb0 ? 1 : 0, k0 = (kb - (seg ? p.kb0 : 0)) * kPerBlock;
+                    const CUtensorMap* ma = &p.a[seg];
+                    const CUtensorMap* mb = &p.b[MODE == kGated ? (int)half : seg];
+                    if (g.a_mn) {
+                        load_box(sa, ma, m0, k0, bar);
+                        load_box(sa + 8192, ma, m0 + 64, k0, bar);
+                    } else {
+                        load_box(sa, ma, k0, m0, bar);
+                    }
+                    if (g.b_mn) {
+                        load_box(sb, mb, n0, k0, bar);
+                        if (BN == 256) load_box(sb + 8192, mb, n0 + 64, k0, bar);
+                    } else {
+                        load_box(sb, mb, k0, n0, bar);
+                    }
+                    if (++s == S::kStages) s = 0, ph ^= 1u;
+                }
+            }
+            if (!ok) {
+                atomicExch(g.status, 1);
+                for (const long long t0 = clock64(); clock64() - t0 < 200000;) {}   // copies on their way land before the CTA ends
+            }
+        }
+    } else if (warp == 1) {
+        if (half == 0) {
+            const unsigned leader = elect();
+            const unsigned short mask = (unsigned short)(3u << lead_rank);
+            int s = 0, as = 0;
+            unsigned ph = 0, aph = 0;
+            bool ok = true;
+            const unsigned long long da = operand_desc(0, g.a_mn, 8192), db = operand_desc(0, g.b_mn, 8192);
+            const unsigned a_step = g.a_mn ? 128u : 2u, b_step = g.b_mn ? 128u : 2u;
+            for (int t = cluster; t < g.tiles && ok; t += clusters) {
+                const Tile at = tile_of(t);
+                if (!(ok = bar_wait(b_acc_empty + 8 * as, aph ^ 1u, g.wait))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const unsigned d = tmem + (unsigned)(as * BN);
+                unsigned add = 0;
+                for (int kb = kb_begin(*at.p), e = kb_end(*at.p); kb < e; ++kb) {
+                    if (!(ok = bar_wait(b_full + 8 * s, ph, g.wait))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    // (an address carries the CTA's rank above its 18 bits, which must not reach the descriptor's strides)
+                    const unsigned sa = ((s_stage + (unsigned)(s * S::kStageBytes)) & 0x3FFFFu) >> 4, sb = sa + (S::kABytes >> 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        mma_pair<MODE == kInt8>(leader, d, da + (sa + a_step * i), db + (sb + b_step * i), g.idesc, add);
+                        add = 1;
+                    }
+                    commit_pair(leader, b_empty + 8 * s, mask);
+                    if (++s == S::kStages) s = 0, ph ^= 1u;
+                }
+                if (!ok) break;
+                commit_pair(leader, b_acc_full + 8 * as, mask);
+                as ^= 1;
+                if (!as) aph ^= 1u;
+            }
+            if (!ok && leader) atomicExch(g.status, 2);
+        }
+    }
+
+    __syncwarp();
+
+    // ---- epilogue ---------------------------------------------------------------------------------------------------
+    const int quad = warp & 3, side = (warp - 4) >> 2;   // 32 accumulator rows; every other unit of columns
+    const unsigned patch = s_out + (unsigned)((warp - 4) * S::kStagingBytes);
+    auto acc_cols = [&](int u, int j) { return MODE == kGated ? j * (BN / 2) + u * 32 : u * S::kUnitAcc + j * 32; };
+    auto read_unit = [&](int as, int u, unsigned* acc) {
+        const unsigned d = tmem + (unsigned)(as * BN) + ((unsigned)(quad * 32) << 16);
+#pragma unroll
+        for (int j = 0; j < S::kUnitAcc / 32; ++j) tmem_ld32(d + (unsigned)acc_cols(u, j), acc + 32 * j);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    };
+    // what a unit needs besides its sums
+    auto fetch = [&](const Tile& at, int u, uint4* e) {
+        const int row = at.mt * 256 + (int)half * 128 + quad * 32 + lane, col = at.nt * S::kTileN + u * S::kUnitCols;
+        if constexpr (MODE == kGateGrad) {
+            fetch32<T>(g.e0, g.e_ld, row, at.p->M, col, at.p->N, e);
+            fetch32<T>(g.e1, g.e1_ld, row, at.p->M, col, at.p->N, e + 4);
+        }
+        if constexpr (MODE == kInt8) {
+            if (g.e0) fetch32<T>(g.e0, g.e_ld, row, at.p->M, col, at.p->N, e);
+        }
+    };
+    auto finish = [&](const Tile& at, int u, unsigned* acc, const uint4* e) {
+        const GemmProblem& p = *at.p;
+        const int row0 = at.mt * 256 + (int)half * 128 + quad * 32, col = at.nt * S::kTileN + u * S::kUnitCols;
+        if (row0 >= p.M || col >= p.N) return;   // (the same for all lanes)
+        float* v = reinterpret_cast<float*>(acc);
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the patch is free
+        __syncwarp();
+        if constexpr (MODE == kPlain) {
+            stage_row<T, 64>(patch, lane, v);
+        } else if constexpr (MODE == kGated) {
+            if (g.save) {
+                stage_row<T, 32>(patch + S::kOutRow * 32, lane, v);
+                stage_row<T, 32>(patch + 2 * S::kOutRow * 32, lane, v + 32);
+            }
+            with_act(g.act, [&](auto act) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = act_of<decltype(act)::value>(v[j]) * v[32 + j];
+            });
+            stage_row<T, 32>(patch, lane, v);
+        } else if constexpr (MODE == kGateGrad) {
+            with_act(g.act, [&](auto act) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {   // a 16-byte piece of each output at a time
+                    float h[8], dg[8], du[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float gv = value_of<T>(e, j + i), uv = value_of<T>(e + 4, j + i);
+                        float slope;
+                        const float a = act_slope<decltype(act)::value>(gv, &slope);
+                        dg[i] = v[j + i] * uv * slope;
+                        du[i] = v[j + i] * a;
+                        h[i] = a * uv;
+                    }
+                    stage_piece<T>(patch, lane, j / 8, h);
+                    stage_piece<T>(patch + S::kOutRow * 32, lane, j / 8, dg);
+                    stage_piece<T>(patch + 2 * S::kOutRow * 32, lane, j / 8, du);
+                }
+            });
+        } else {
+            const int row = row0 + lane;
+            const float rs = row < p.M ? g.row_scale[row] : 0.f;
+            const bool whole = col + 32 <= p.N;
+            with_act(g.act, [&](auto act) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    float cs[4], bs[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (whole) {
+                        *reinterpret_cast<float4*>(cs) = *reinterpret_cast<const float4*>(g.col_scale + col + j);
+                        if (g.bias) *reinterpret_cast<float4*>(bs) = *reinterpret_cast<const float4*>(g.bias + col + j);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bool in = col + j + i < p.N;
+                            cs[i] = in ? g.col_scale[col + j + i] : 0.f;
+                            if (g.bias) bs[i] = in ? g.bias[col + j + i] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float r = g.e0 ? value_of<T>(e, j + i) : 0.f;
+                        v[j + i] = i8_value<decltype(act)::value>((int)acc[j + i], rs, cs[i], bs[i], r, g.res_after);
+                    }
+                }
+            });
+            stage_row<T, 32>(patch, lane, v);
+        }
+        if (col + S::kUnitCols > p.N && p.N % (16 / (int)sizeof(T)) != 0) {
+            __syncwarp();
+            unstage_row<T, S::kUnitCols>(patch, lane, p.op[0], p.o_ld[0], row0 + lane, p.M, col, p.N);
+            if ((MODE == kGated && g.save) || MODE == kGateGrad) {
+                unstage_row<T, S::kUnitCols>(patch + S::kOutRow * 32, lane, p.op[1], p.o_ld[1], row0 + lane, p.M, col, p.N);
+                unstage_row<T, S::kUnitCols>(patch + 2 * S::kOutRow * 32, lane, p.op[2], p.o_ld[2], row0 + lane, p.M, col, p.N);
+            }
+            return;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            store_box(&p.o[0], col, row0, patch);
+            if ((MODE == kGated && g.save) || MODE == kGateGrad) {
+                store_box(&p.o[1], col, row0, patch + S::kOutRow * 32);
+                store_box(&p.o[2], col, row0, patch + 2 * S::kOutRow * 32);
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    };
+
+    bool ok = true;
+    if (warp >= 4 && KS == 1) {
+        int as = 0;
+        unsigned aph = 0;
+        for (int t = cluster; t < g.tiles; t += clusters) {
+            const Tile at = tile_of(t);
+            uint4 e[8], e_next[8];
+            fetch(at, side, e);
+            if (!(ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full + 8 * as, aph, g.wait)))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+            for (int u = side; u < S::kUnits; u += 2) {
+                unsigned acc[S::kUnitAcc];
+                read_unit(as, u, acc);
+                if (u + 2 < S::kUnits) fetch(at, u + 2, e_next);
+                else {   // all sums of this tile are in registers: the pair may overwrite them
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0)
+                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(b_acc_empty + 8 * as, lead_rank)) : "memory");
+                }
+                finish(at, u, acc, e);
+                if constexpr (MODE == kGateGrad || MODE == kInt8) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) e[j] = e_next[j];
+                }
+            }
+            as ^= 1;
+            if (!as) aph ^= 1u;
+        }
+    }
+    if (KS > 1) {
+        // One tile a cluster.  Behind the first barrier every pair's products are complete, so the operand rings are free and
+        // take the other pairs' sums: unit u belongs to the pair u * KS / kUnits.
+        const Tile at = tile_of(cluster);
+        if (warp >= 4) {
+            ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full, 0, g.wait));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
+        __syncthreads();
+        cluster_barrier();
+        constexpr unsigned kSlot = 32 * S::kUnitAcc * 4;   // a warp's sums of a unit
+        const int per = S::kUnits / KS;
+        auto slot = [&](int u, unsigned from) { return s_stage + ((unsigned)((u % per) * KS + (int)from) * 4u + (unsigned)quad) * kSlot + (unsigned)lane * 16u; };
+        if (warp >= 4 && ok) {
+#pragma unroll 1
+            for (int u = side; u < S::kUnits; u += 2) {
+                const unsigned owner = (unsigned)(u / per);
+                if (owner == share) continue;
+                unsigned acc[S::kUnitAcc];
+                read_unit(0, u, acc);
+                const unsigned to = at_rank(slot(u, share), 2 * owner + half);
+#pragma unroll
+                for (int j = 0; j < S::kUnitAcc / 4; ++j) st_cluster16(to + j * 512, acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+            }
+        }
+        __syncthreads();
+        cluster_barrier();
+        if (warp >= 4 && ok) {
+#pragma unroll 1
+            for (int u = (int)share * per; u < ((int)share + 1) * per; ++u) {
+                if ((u & 1) != side && per > 1) continue;
+                if (per == 1 && side != 0) continue;
+                uint4 e[8];
+                fetch(at, u, e);
+                unsigned acc[S::kUnitAcc];
+                read_unit(0, u, acc);
+                // shares are added in their order, whichever pair adds them
+                unsigned sum[S::kUnitAcc];
+#pragma unroll
+                for (int j = 0; j < S::kUnitAcc; ++j) sum[j] = 0u;
+#pragma unroll 1
+                for (unsigned from = 0; from < (unsigned)KS; ++from) {
+#pragma unroll
+                    for (int j = 0; j < S::kUnitAcc / 4; ++j) {
+                        uint4 w = make_uint4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+                        if (from != share) w = ld_shared16(slot(u, from) + j * 512);
+                        const unsigned* we = reinterpret_cast<const unsigned*>(&w);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (MODE == kInt8) sum[4 * j + i] += we[i];
+                            else sum[4 * j + i] = __float_as_uint(__uint_as_float(sum[4 * j + i]) + __uint_as_float(we[i]));
+                        }
+                    }
+                }
+                finish(at, u, sum, e);
+            }
+        }
+    }
+    if (warp >= 4) {
+        if (!ok && lane == 0) atomicExch(g.status, 3);
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_barrier();   // no CTA of the cluster leaves, or gives up its TMEM, while another still works on its memory
+    if (warp == 2) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");
+    }
+}
+
+}  // namespace rtoss_tok
+
+#endif
