@@ -85,7 +85,7 @@ struct GemmShape {
     static constexpr int kUnits = BN / kUnitAcc;
     static constexpr int kOutRow = kUnitCols * (int)sizeof(T);                     // bytes of a staged output row: 64 or 128
     static constexpr int kOuts = MODE == kGated || MODE == kGateGrad ? 3 : 1;
-    static constexpr int kStagingBytes = kOutRow * 32 * kOuts;                     // of a warp
+    static constexpr int kStagingBytes = kOutRow * 32 * kOuts + (MODE == kInt8 ? 1024 : 0);                     // of a warp
     static constexpr int kRoom = 226 * 1024 - kEpiWarps * kStagingBytes;
     static constexpr int kStages = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
     static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 256;
@@ -459,7 +459,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             if (g.e0) fetch32<T>(g.e0, g.e_ld, row, at.p->M, col, at.p->N, e);
         }
     };
-    auto finish = [&](const Tile& at, int u, unsigned* acc, const uint4* e) {
+    // kInt8: the scale of this lane's row, and the scale and bias of the unit's column `lane`
+    auto row_of = [&](const Tile& at) {
+        const int row = at.mt * 256 + (int)half * 128 + quad * 32 + lane;
+        return MODE == kInt8 && row < at.p->M ? g.row_scale[row] : 0.f;
+    };
+    auto column_of = [&](const Tile& at, int u) {
+        float2 cb = make_float2(0.f, 0.f);
+        const int col = at.nt * S::kTileN + u * S::kUnitCols + lane;
+        if (MODE == kInt8 && col < at.p->N) {
+            cb.x = g.col_scale[col];
+            if (g.bias) cb.y = g.bias[col];
+        }
+        return cb;
+    };
+    auto finish = [&](const Tile& at, int u, unsigned* acc, const uint4* e, float row_scale, float2 cb) {
         const GemmProblem& p = *at.p;
         const int row0 = at.mt * 256 + (int)half * 128 + quad * 32, col = at.nt * S::kTileN + u * S::kUnitCols;
         if (row0 >= p.M || col >= p.N) return;   // (the same for all lanes)
@@ -498,29 +512,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                 }
             });
         } else {
-            const int row = row0 + lane;
-            const float rs = row < p.M ? g.row_scale[row] : 0.f;
-            const bool whole = col + 32 <= p.N;
+            // the unit's column scales and biases: a lane fetches one of each, all lanes read all
+            const unsigned cols_at = patch + S::kOutRow * 32;
+            __syncwarp();
+            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(cols_at + 8u * (unsigned)lane), "f"(cb.x), "f"(cb.y) : "memory");
+            __syncwarp();
             with_act(g.act, [&](auto act) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    float cs[4], bs[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (whole) {
-                        *reinterpret_cast<float4*>(cs) = *reinterpret_cast<const float4*>(g.col_scale + col + j);
-                        if (g.bias) *reinterpret_cast<float4*>(bs) = *reinterpret_cast<const float4*>(g.bias + col + j);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const bool in = col + j + i < p.N;
-                            cs[i] = in ? g.col_scale[col + j + i] : 0.f;
-                            if (g.bias) bs[i] = in ? g.bias[col + j + i] : 0.f;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float r = g.e0 ? value_of<T>(e, j + i) : 0.f;
-                        v[j + i] = i8_value<decltype(act)::value>((int)acc[j + i], rs, cs[i], bs[i], r, g.res_after);
-                    }
+                for (int j = 0; j < 32; j += 2) {
+                    const uint4 w = ld_shared16(cols_at + 8u * j);
+                    const float r0 = g.e0 ? value_of<T>(e, j) : 0.f, r1 = g.e0 ? value_of<T>(e, j + 1) : 0.f;
+                    v[j] = i8_value<decltype(act)::value>((int)acc[j], row_scale, __uint_as_float(w.x), __uint_as_float(w.y), r0, g.res_after);
+                    v[j + 1] = i8_value<decltype(act)::value>((int)acc[j + 1], row_scale, __uint_as_float(w.z), __uint_as_float(w.w), r1, g.res_after);
                 }
             });
             stage_row<T, 32>(patch, lane, v);
@@ -554,20 +557,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             const Tile at = tile_of(t);
             uint4 e[8], e_next[8];
             fetch(at, side, e);
+            const float rs = row_of(at);
+            float2 cb = column_of(at, side), cb_next = cb;
             if (!(ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full + 8 * as, aph, g.wait)))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int u = side; u < S::kUnits; u += 2) {
                 unsigned acc[S::kUnitAcc];
                 read_unit(as, u, acc);
-                if (u + 2 < S::kUnits) fetch(at, u + 2, e_next);
-                else {   // all sums of this tile are in registers: the pair may overwrite them
+                if (u + 2 < S::kUnits) {
+                    fetch(at, u + 2, e_next);
+                    cb_next = column_of(at, u + 2);
+                } else {   // all sums of this tile are in registers: the pair may overwrite them
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0)
                         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(b_acc_empty + 8 * as, lead_rank)) : "memory");
                 }
-                finish(at, u, acc, e);
+                finish(at, u, acc, e, rs, cb);
+                cb = cb_next;
                 if constexpr (MODE == kGateGrad || MODE == kInt8) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) e[j] = e_next[j];
@@ -631,7 +639,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                         }
                     }
                 }
-                finish(at, u, sum, e);
+                finish(at, u, sum, e, row_of(at), column_of(at, u));
             }
         }
     }

@@ -10,90 +10,119 @@ constexpr const char* kQuant = "quantize rows";
 constexpr const char* kMul = "matmul i8";
 
 // ---- rows to 8 bits -------------------------------------------------------------------------------------------------
-// bound: bytes (a row is read once and one byte a value written).  A group of G threads takes a row and holds up to 32 values
-// a thread in registers between the maximum and the rounding; longer rows are read again, from the caches.
+// bound: bytes (a row is read once and one byte a value written), if the arithmetic stays near six instructions a value: the
+// maximum is taken over the bits as they lie in memory (two 16-bit magnitudes at a time), and one fused multiply-add against
+// 1.5 * 2^23 rounds x / s and leaves the code in its low bits.  G threads take a row and hold up to 32 values each between the
+// maximum and the rounding; longer rows are read again, from the caches.
 constexpr int kHold = 4;   // pieces of eight values a thread holds
 
+template <typename T>
+struct __align__(16) Piece {
+    T e[8];
+};
 // Eight values from element i of a row on (zeros behind its end).
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, int i, int cols, float (&v)[8]) {
+__device__ __forceinline__ void fetch8(const T* row, int i, int cols, Piece<T>& v) {
     if (VEC && i + 8 <= cols) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 p = *reinterpret_cast<const float4*>(row + i), q = *reinterpret_cast<const float4*>(row + i + 4);
-            v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
-        } else {
-            const uint4 p = *reinterpret_cast<const uint4*>(row + i);
-            const T* e = reinterpret_cast<const T*>(&p);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = rtoss_dev::to_f32<T>(e[j]);
-        }
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(&v)[j] = reinterpret_cast<const uint4*>(row + i)[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = i + j < cols ? rtoss_dev::to_f32<T>(row[i + j]) : 0.f;
+        for (int j = 0; j < 8; ++j) v.e[j] = i + j < cols ? row[i + j] : rtoss_dev::from_f32<T>(0.f);
     }
 }
-
-// The code of x: the quotient x / s in fp32, rounded half to even.  The product with 1 / s is within 3e-5 of it, so only
-// values that close to a border need the division.
-__device__ __forceinline__ int code_of(float x, float s, float inv, bool divide) {
-    float q = x * inv, r = rintf(q);
-    if (divide || fabsf(fabsf(q - r) - 0.5f) < 1e-4f) r = rintf(__fdiv_rn(x, s));
-    return (int)fminf(fmaxf(r, -127.f), 127.f);
+// Largest magnitude so far, as bits: magnitudes compare as integers, and Inf and NaN lie above every number.  16-bit types: one in
+// each half of the word.
+template <typename T>
+__device__ __forceinline__ unsigned most_of(unsigned top, const Piece<T>& v) {
+    const unsigned* w = reinterpret_cast<const unsigned*>(&v);
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) * 2; ++j)
+        top = sizeof(T) == 4 ? max(top, w[j] & 0x7FFFFFFFu) : __vmaxu2(top, w[j] & 0x7FFF7FFFu);
+    return top;
 }
 
-// G: threads of a row, 32 (eight rows a block) or 256.
+// The code of x: the quotient x / s in fp32, rounded half to even.
+__device__ __forceinline__ int exact_code(float x, float s) { return (int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f); }
+
+// Eight codes.  x * (1 / s) is within 127 * 2^-23 < 1.6e-5 of the rounded quotient, so its nearest integer is the quotient's
+// unless it lies that close to half way; then (and for scales whose reciprocal would overflow) the division decides.
+template <typename T>
+__device__ __forceinline__ uint2 codes_of(const Piece<T>& v, float s, float inv, bool divide) {
+    constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: the sum's last bit is 1
+    unsigned t[8];
+    float far = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float x = rtoss_dev::to_f32<T>(v.e[j]), m = fmaf(x, inv, kMagic);
+        t[j] = __float_as_uint(m);
+        far = fmaxf(far, fabsf(fmaf(x, inv, kMagic - m)));
+    }
+    if (divide || far > 0.5f - 2e-5f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = (unsigned)exact_code(rtoss_dev::to_f32<T>(v.e[j]), s);
+    }
+    return make_uint2(__byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410));
+}
+
+// G: threads of a row; up to 32 they are part of a warp, else a block.
 template <typename T, bool VEC, int G>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ x, long long x_ld, signed char* __restrict__ q, long long q_ld,
                                                             float* __restrict__ scale, int rows, int cols) {
     rtoss_dev::pdl_enter();
     __shared__ unsigned s_top[8];
-    const int row = G == 32 ? (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5) : (int)blockIdx.x, at = (int)threadIdx.x % G;
-    if (row >= rows) return;   // (a whole warp, or nobody)
+    const int at = (int)threadIdx.x % G;
+    const long long first = G <= 32 ? ((long long)blockIdx.x * 256 + threadIdx.x) / G : blockIdx.x;
+    const bool here = first < rows;   // (whole groups of G; a warp stays together for its shuffles)
+    const int row = here ? (int)first : rows - 1;
     const T* xr = x + (long long)row * x_ld;
-    float v[kHold][8];
+    Piece<T> v[kHold];
     unsigned top = 0u;
 #pragma unroll
     for (int p = 0; p < kHold; ++p) {
         const int i = (p * G + at) * 8;
-        if (i < cols) load8<T, VEC>(xr, i, cols, v[p]);
+        if (i < cols) fetch8<T, VEC>(xr, i, cols, v[p]);
         else
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[p][j] = 0.f;
+            for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(&v[p])[j] = make_uint4(0u, 0u, 0u, 0u);
     }
-    // magnitudes compare as integers, and Inf and NaN lie above every number
 #pragma unroll
-    for (int p = 0; p < kHold; ++p)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[p][j]) & 0x7FFFFFFFu);
+    for (int p = 0; p < kHold; ++p) top = most_of<T>(top, v[p]);
     for (int i = (kHold * G + at) * 8; i < cols; i += G * 8) {
-        float w[8];
-        load8<T, VEC>(xr, i, cols, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(w[j]) & 0x7FFFFFFFu);
+        Piece<T> w;
+        fetch8<T, VEC>(xr, i, cols, w);
+        top = most_of<T>(top, w);
     }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (sizeof(T) == 2) top = max(top >> 16, top & 0xFFFFu);
+    if (G >= 32) top = __reduce_max_sync(0xFFFFFFFFu, top);
+    else
+#pragma unroll
+        for (int o = G / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     if (G > 32) {
         if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 8; ++w) top = max(top, s_top[w]);
+        for (int w = 0; w < G / 32; ++w) top = max(top, s_top[w]);
     }
-    const bool finite = top < 0x7F800000u;
-    const float s = finite ? __fdiv_rn(__uint_as_float(top), 127.f) : __int_as_float(0x7FC00000);
+    float most = __uint_as_float(top);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) most = __uint_as_float(top << 16);
+    if constexpr (std::is_same<T, __half>::value) most = __half2float(__ushort_as_half((unsigned short)top));
+    const bool finite = most < __int_as_float(0x7F800000);   // (false for NaN)
+    const float s = finite ? __fdiv_rn(most, 127.f) : __int_as_float(0x7FC00000);
+    if (!here) return;
     if (at == 0) scale[row] = s;
     const bool live = finite && s > 0.f, divide = !(s > 1e-30f);
     const float inv = live ? __fdiv_rn(1.f, s) : 0.f;
     signed char* qr = q + (long long)row * q_ld;
     const bool vec_out = (reinterpret_cast<unsigned long long>(qr) & 7u) == 0;
-    auto put = [&](int i, const float (&w)[8]) {
-        unsigned b[2] = {0u, 0u};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j / 4] |= (unsigned)(unsigned char)(signed char)(live ? code_of(w[j], s, inv, divide) : 0) << (8 * (j & 3));
-        if (vec_out && i + 8 <= cols) *reinterpret_cast<uint2*>(qr + i) = make_uint2(b[0], b[1]);
+    auto put = [&](int i, const Piece<T>& w) {
+        const uint2 b = live ? codes_of<T>(w, s, inv, divide) : make_uint2(0u, 0u);
+        if (vec_out && i + 8 <= cols) *reinterpret_cast<uint2*>(qr + i) = b;
         else
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (i + j < cols) qr[i + j] = (signed char)(b[j / 4] >> (8 * (j & 3)));
+                if (i + j < cols) qr[i + j] = (signed char)((j < 4 ? b.x : b.y) >> (8 * (j & 3)));
     };
 #pragma unroll
     for (int p = 0; p < kHold; ++p) {
@@ -101,23 +130,30 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict_
         if (i < cols) put(i, v[p]);
     }
     for (int i = (kHold * G + at) * 8; i < cols; i += G * 8) {
-        float w[8];
-        load8<T, VEC>(xr, i, cols, w);
+        Piece<T> w;
+        fetch8<T, VEC>(xr, i, cols, w);
         put(i, w);
     }
 }
 
+// As few threads as hold a row, so that each has several loads in flight; a block of 128 or 256 for rows of more than 1024 values.
+template <typename T, bool VEC>
+int quantize_as(const T* x, long long x_ld, signed char* q, long long q_ld, float* scale, int rows, int cols, cudaStream_t s) {
+    auto go = [&](auto kernel, int g) {
+        const unsigned grid = g <= 32 ? (unsigned)(((long long)rows * g + 255) / 256) : (unsigned)rows;
+        return (int)rtoss_dev::launch_pdl(kernel, grid, (unsigned)(g <= 32 ? 256 : g), 0, s, x, x_ld, q, q_ld, scale, rows, cols);
+    };
+    if (cols <= 128) return go(quantize_rows_kernel<T, VEC, 4>, 4);
+    if (cols <= 512) return go(quantize_rows_kernel<T, VEC, 16>, 16);
+    if (cols <= 1024) return go(quantize_rows_kernel<T, VEC, 32>, 32);
+    if (cols <= 4096) return go(quantize_rows_kernel<T, VEC, 128>, 128);
+    return go(quantize_rows_kernel<T, VEC, 256>, 256);
+}
+
 template <typename T>
 int quantize(const void* x, int64_t x_ld, int8_t* q, int64_t q_ld, float* scale, int rows, int cols, cudaStream_t s) {
-    const bool vec = aligned16(x) && (x_ld * (int64_t)sizeof(T)) % 16 == 0;
-    const T* xt = (const T*)x;
-    if (cols <= 1024) {   // one warp holds a row
-        const unsigned grid = (unsigned)((rows + 7) / 8);
-        return vec ? (int)rtoss_dev::launch_pdl(quantize_rows_kernel<T, true, 32>, grid, 256, 0, s, xt, (long long)x_ld, (signed char*)q, (long long)q_ld, scale, rows, cols)
-                   : (int)rtoss_dev::launch_pdl(quantize_rows_kernel<T, false, 32>, grid, 256, 0, s, xt, (long long)x_ld, (signed char*)q, (long long)q_ld, scale, rows, cols);
-    }
-    return vec ? (int)rtoss_dev::launch_pdl(quantize_rows_kernel<T, true, 256>, (unsigned)rows, 256, 0, s, xt, (long long)x_ld, (signed char*)q, (long long)q_ld, scale, rows, cols)
-               : (int)rtoss_dev::launch_pdl(quantize_rows_kernel<T, false, 256>, (unsigned)rows, 256, 0, s, xt, (long long)x_ld, (signed char*)q, (long long)q_ld, scale, rows, cols);
+    return aligned16(x) && (x_ld * (int64_t)sizeof(T)) % 16 == 0 ? quantize_as<T, true>((const T*)x, x_ld, (signed char*)q, q_ld, scale, rows, cols, s)
+                                                                 : quantize_as<T, false>((const T*)x, x_ld, (signed char*)q, q_ld, scale, rows, cols, s);
 }
 
 // ---- the product ----------------------------------------------------------------------------------------------------

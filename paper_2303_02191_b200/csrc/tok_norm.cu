@@ -37,37 +37,48 @@ struct NormArgs {
 };
 
 // ---- eight values -----------------------------------------------------------------------------------------------------
+// As they lie in memory: a row's loads stay in flight until its values are widened.
 template <typename T>
-__device__ __forceinline__ void load8(const void* base, long long ld, int row, int i, int D, bool vec, float (&v)[8]) {
+struct __align__(16) Raw {
+    T e[8];
+};
+// (VEC: rows and pieces are multiples of 16 bytes)
+template <typename T, bool VEC>
+__device__ __forceinline__ void fetch8(const void* base, long long ld, int row, int i, int D, Raw<T>& r) {
     const T* at = reinterpret_cast<const T*>(base) + (long long)row * ld + i;
-    if (vec) {   // (then D is a multiple of eight)
-        if constexpr (sizeof(T) == 4) {
-            const float4 p = *reinterpret_cast<const float4*>(at), q = *reinterpret_cast<const float4*>(at + 4);
-            v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
-        } else {
-            const uint4 p = *reinterpret_cast<const uint4*>(at);
-            const T* e = reinterpret_cast<const T*>(&p);
+    if (VEC) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = to_f32<T>(e[j]);
-        }
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(&r)[j] = reinterpret_cast<const uint4*>(at)[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = i + j < D ? to_f32<T>(at[j]) : 0.f;
+        for (int j = 0; j < 8; ++j) r.e[j] = i + j < D ? at[j] : from_f32<T>(0.f);
     }
 }
 template <typename T>
-__device__ __forceinline__ void store8(void* base, long long ld, int row, int i, int D, bool vec, const float (&v)[8]) {
-    T* at = reinterpret_cast<T*>(base) + (long long)row * ld + i;
-    if (vec) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            __align__(16) T e[8];
+__device__ __forceinline__ void zero8(Raw<T>& r) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(v[j]);
-            *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(e);
-        }
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(&r)[j] = make_uint4(0u, 0u, 0u, 0u);
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw<T>& r, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = to_f32<T>(r.e[j]);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const void* base, long long ld, int row, int i, int D, float (&v)[8]) {
+    Raw<T> r;
+    fetch8<T, VEC>(base, ld, row, i, D, r);
+    widen8<T>(r, v);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(void* base, long long ld, int row, int i, int D, const float (&v)[8]) {
+    T* at = reinterpret_cast<T*>(base) + (long long)row * ld + i;
+    if (VEC) {
+        Raw<T> r;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r.e[j] = from_f32<T>(v[j]);
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(at)[j] = reinterpret_cast<const uint4*>(&r)[j];
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -136,13 +147,12 @@ __device__ __forceinline__ void stats(Reduce<G>& red, const float (&v)[P][8], co
 // Threads of a unit, units of a block: G = 32 has eight warps to a block, each a unit.
 template <int G> constexpr int block_of() { return G == 32 ? 256 : G; }
 
-template <typename T, int G, int P>
+template <typename T, bool VEC, int G, int P>
 __global__ void __launch_bounds__(block_of<G>()) norm_forward_kernel(const NormArgs a) {
     __shared__ float buf[4 * (G / 32)];
     const int at = (int)threadIdx.x % G, unit = G == 32 ? (int)blockIdx.x * 8 + (int)threadIdx.x / 32 : (int)blockIdx.x;
     Reduce<G> red{buf, 0, at / 32, (int)threadIdx.x & 31};
     const int D = a.D;
-    const bool vec = a.vec;
     rtoss_dev::pdl_enter();
     const int row0 = unit * a.per_unit, row1 = min(a.rows, row0 + a.per_unit);
     if (row0 >= row1) return;   // (a whole unit)
@@ -160,28 +170,34 @@ __global__ void __launch_bounds__(block_of<G>()) norm_forward_kernel(const NormA
         }
     }
     int gate_row = -1;
-    float y[P][8], r[P][8], y_next[P][8], r_next[P][8];
-    auto load = [&](int row, float (&yv)[P][8], float (&rv)[P][8]) {
+    float y[P][8], r[P][8];
+    Raw<T> yn[P], rn[P];   // of the next row
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        zero8(yn[p]);
+        zero8(rn[p]);
+    }
+    auto fetch = [&](int row) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (in[p]) {
+                fetch8<T, VEC>(a.y, a.y_ld, row, (p * G + at) * 8, D, yn[p]);
+                fetch8<T, VEC>(a.r, a.r_ld, row, (p * G + at) * 8, D, rn[p]);
+            }
+    };
+    fetch(row0);
+    for (int row = row0; row < row1; ++row) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int i = (p * G + at) * 8;
-            if (in[p]) {
-                load8<T>(a.y, a.y_ld, row, i, D, vec, yv[p]);
-                load8<T>(a.r, a.r_ld, row, i, D, vec, rv[p]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) yv[p][j] = rv[p][j] = 0.f;
-            }
+            widen8<T>(yn[p], y[p]);
+            widen8<T>(rn[p], r[p]);
         }
-    };
-    load(row0, y, r);
-    for (int row = row0; row < row1; ++row) {
-        if (row + 1 < row1) load(row + 1, y_next, r_next);
+        if (row + 1 < row1) fetch(row + 1);
         if (a.gate && row / a.S != gate_row) {
             gate_row = row / a.S;
 #pragma unroll
             for (int p = 0; p < P; ++p)
-                if (in[p]) load8<T>(a.gate, a.gate_ld, gate_row, (p * G + at) * 8, D, vec, gate[p]);
+                if (in[p]) load8<T, VEC>(a.gate, a.gate_ld, gate_row, (p * G + at) * 8, D, gate[p]);
         }
         float mean = 0.f, rstd = 1.f;
         if (a.post != RTOSS_NORM_NONE) stats<P, G>(red, y, in, at, D, a.post, a.eps, &mean, &rstd);
@@ -194,30 +210,25 @@ __global__ void __launch_bounds__(block_of<G>()) norm_forward_kernel(const NormA
             }
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (in[p]) store8<T>(a.z, a.z_ld, row, (p * G + at) * 8, D, vec, y[p]);
+            if (in[p]) store8<T, VEC>(a.z, a.z_ld, row, (p * G + at) * 8, D, y[p]);
         if (a.pre != RTOSS_NORM_NONE) {
             stats<P, G>(red, y, in, at, D, a.pre, a.eps, &mean, &rstd);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[p][j] = (y[p][j] - mean) * rstd * wpre[p][j];
-                if (in[p]) store8<T>(a.n, a.n_ld, row, (p * G + at) * 8, D, vec, y[p]);
+                if (in[p]) store8<T, VEC>(a.n, a.n_ld, row, (p * G + at) * 8, D, y[p]);
             }
         }
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[p][j] = y_next[p][j], r[p][j] = r_next[p][j];
     }
 }
 
-template <typename T, int G, int P>
+template <typename T, bool VEC, int G, int P>
 __global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const NormArgs a) {
     __shared__ float buf[4 * (G / 32)];
     const int at = (int)threadIdx.x % G, unit = G == 32 ? (int)blockIdx.x * 8 + (int)threadIdx.x / 32 : (int)blockIdx.x;
     Reduce<G> red{buf, 0, at / 32, (int)threadIdx.x & 31};
     const int D = a.D;
-    const bool vec = a.vec;
     rtoss_dev::pdl_enter();
     const int row0 = unit * a.per_unit, row1 = min(a.rows, row0 + a.per_unit);
     if (row0 >= row1) return;
@@ -238,24 +249,40 @@ __global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const Norm
     }
     int gate_row = -1;
     float y[P][8], r[P][8], dz[P][8], dn[P][8];
+    Raw<T> yn[P], rn[P], dzn[P], dnn[P];   // of the next row
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        zero8(yn[p]);
+        zero8(rn[p]);
+        zero8(dzn[p]);
+        zero8(dnn[p]);
+    }
+    auto fetch = [&](int row) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (in[p]) {
+                const int i = (p * G + at) * 8;
+                fetch8<T, VEC>(a.y, a.y_ld, row, i, D, yn[p]);
+                fetch8<T, VEC>(a.r, a.r_ld, row, i, D, rn[p]);
+                if (a.dz) fetch8<T, VEC>(a.dz, a.dz_ld, row, i, D, dzn[p]);
+                if (a.dn) fetch8<T, VEC>(a.dn, a.dn_ld, row, i, D, dnn[p]);
+            }
+    };
+    fetch(row0);
     for (int row = row0; row < row1; ++row) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int i = (p * G + at) * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[p][j] = r[p][j] = dz[p][j] = dn[p][j] = 0.f;
-            if (in[p]) {
-                load8<T>(a.y, a.y_ld, row, i, D, vec, y[p]);
-                load8<T>(a.r, a.r_ld, row, i, D, vec, r[p]);
-                if (a.dz) load8<T>(a.dz, a.dz_ld, row, i, D, vec, dz[p]);
-                if (a.dn) load8<T>(a.dn, a.dn_ld, row, i, D, vec, dn[p]);
-            }
+            widen8<T>(yn[p], y[p]);
+            widen8<T>(rn[p], r[p]);
+            widen8<T>(dzn[p], dz[p]);
+            widen8<T>(dnn[p], dn[p]);
         }
+        if (row + 1 < row1) fetch(row + 1);
         if (a.gate && row / a.S != gate_row) {
             gate_row = row / a.S;
 #pragma unroll
             for (int p = 0; p < P; ++p)
-                if (in[p]) load8<T>(a.gate, a.gate_ld, gate_row, (p * G + at) * 8, D, vec, gate[p]);
+                if (in[p]) load8<T, VEC>(a.gate, a.gate_ld, gate_row, (p * G + at) * 8, D, gate[p]);
         }
         // v and z again
         float ymean = 0.f, yrstd = 1.f, zmean = 0.f, zrstd = 1.f;
@@ -303,7 +330,7 @@ __global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const Norm
                 m[0] += dz[p][j] * y[p][j];
                 m[1] += (p * G + at) * 8 + j < D ? dz[p][j] : 0.f;
             }
-            if (in[p]) store8<T>(a.dr, a.dr_ld, row, (p * G + at) * 8, D, vec, out);
+            if (in[p]) store8<T, VEC>(a.dr, a.dr_ld, row, (p * G + at) * 8, D, out);
         }
         if (a.post != RTOSS_NORM_NONE) {
             red.template sum<2>(m);
@@ -315,7 +342,7 @@ __global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const Norm
         }
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (in[p]) store8<T>(a.dy, a.dy_ld, row, (p * G + at) * 8, D, vec, dz[p]);
+            if (in[p]) store8<T, VEC>(a.dy, a.dy_ld, row, (p * G + at) * 8, D, dz[p]);
         // a gate's last row here: its sum is final when all its rows were this unit's, else one of the unit's two shares
         if (a.dgate && (row + 1 == row1 || (row + 1) / a.S != row / a.S)) {
             const int first = row / a.S * a.S, last = first + a.S;   // (S divides the tokens)
@@ -325,8 +352,8 @@ __global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const Norm
             for (int p = 0; p < P; ++p) {
                 const int i = (p * G + at) * 8;
                 if (in[p]) {
-                    if (whole) store8<T>(a.dgate, a.dgate_ld, row / a.S, i, D, vec, s_gate[p]);
-                    else store8<float>(part, 0, 0, i, D, vec, s_gate[p]);
+                    if (whole) store8<T, VEC>(a.dgate, a.dgate_ld, row / a.S, i, D, s_gate[p]);
+                    else store8<float, VEC>(part, 0, 0, i, D, s_gate[p]);
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s_gate[p][j] = 0.f;
@@ -337,8 +364,8 @@ __global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const Norm
     for (int p = 0; p < P; ++p) {
         const int i = (p * G + at) * 8;
         if (!in[p]) continue;
-        if (a.p_post) store8<float>(a.p_post, D, unit, i, D, vec, s_post[p]);
-        if (a.p_pre) store8<float>(a.p_pre, D, unit, i, D, vec, s_pre[p]);
+        if (a.p_post) store8<float, VEC>(a.p_post, D, unit, i, D, s_post[p]);
+        if (a.p_pre) store8<float, VEC>(a.p_pre, D, unit, i, D, s_pre[p]);
     }
 }
 
@@ -455,13 +482,14 @@ struct JoinArgs {
     float *dpost, *dpre;
     void* dgate;
     long long dgate_ld;
-    int D, units, per_unit, S;
+    int D, units, per_unit, S, by_gate;
 };
 
-// 32 columns a block, eight runs of units side by side, joined in their order.
+// 32 columns a block, 32 runs of units side by side, joined in their order.
+constexpr int kJoinRuns = 32;
 template <typename T>
-__global__ void __launch_bounds__(256) norm_join_kernel(const JoinArgs a) {
-    __shared__ float s[8][32];
+__global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArgs a) {
+    __shared__ float s[kJoinRuns][32];
     rtoss_dev::pdl_enter();
     const int col = (int)blockIdx.x * 32 + ((int)threadIdx.x & 31), run = (int)threadIdx.x >> 5, what = (int)blockIdx.y;
     const bool in = col < a.D;
@@ -470,20 +498,22 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const JoinArgs a) {
     long long pitch = a.D;
     long long row0 = 0;   // first row of the gate
     if (what >= 2) {
-        // the gate that runs across the end of unit what - 2, at the first such end (a gate of one unit is written already)
+        // gates that run across the end of a unit (the others are written already), counted by gate or, where there are fewer
+        // of them, by the unit whose end is a gate's first such end
         const long long end = (long long)(what - 1) * a.per_unit;
-        row0 = end / a.S * a.S;
+        row0 = a.by_gate ? (long long)(what - 2) * a.S : end / a.S * a.S;
         first = (int)(row0 / a.per_unit);
         last = (int)((row0 + a.S - 1) / a.per_unit) + 1;
-        if (row0 == end || first != what - 2) return;
+        if (last - first == 1 || (!a.by_gate && (row0 == end || first != what - 2))) return;
         p = a.p_gate;
         pitch = 2ll * a.D;
     } else if (!p) {
         return;
     }
-    const int each = (last - first + 7) / 8, lo = first + run * each, hi = min(last, lo + each);
+    const int each = (last - first + kJoinRuns - 1) / kJoinRuns, lo = first + run * each, hi = min(last, lo + each);
     float sum = 0.f;
     if (in)
+#pragma unroll 4
         for (int u = lo; u < hi; ++u) {
             // (a gate that begins inside a unit is that unit's second share)
             const long long second = what >= 2 && row0 > (long long)u * a.per_unit ? a.D : 0;
@@ -494,7 +524,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const JoinArgs a) {
     if (run == 0 && in) {
         sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum += s[k][threadIdx.x & 31];
+        for (int k = 0; k < kJoinRuns; ++k) sum += s[k][threadIdx.x & 31];
         if (what == 0) a.dpost[col] = sum;
         else if (what == 1) a.dpre[col] = sum;
         else reinterpret_cast<T*>(a.dgate)[row0 / a.S * a.dgate_ld + col] = from_f32<T>(sum);
@@ -506,7 +536,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const JoinArgs a) {
 struct Plan {
     int G, P, units, per_unit;
 };
-Plan plan_of(int64_t rows, int D, int sms) {
+Plan plan_of(int64_t rows, int D, int sms, bool backward) {
     Plan p;
     if (D <= 256) p.G = 32, p.P = 1;
     else if (D <= 1024) p.G = 128, p.P = 1;
@@ -514,30 +544,35 @@ Plan plan_of(int64_t rows, int D, int sms) {
     else if (D <= 4096) p.G = 512, p.P = 1;
     else if (D <= 8192) p.G = 512, p.P = 2;
     else p.G = kLongThreads, p.P = 0;
-    const int64_t most = (int64_t)sms * (p.G == 32 ? 16 : 1024 / p.G);
+    const int64_t most = (int64_t)sms * (backward ? (p.G == 32 ? 16 : p.G == 128 ? 4 : p.G == 256 ? 2 : 1) : p.G == 32 ? 32 : 1024 / p.G);
     const int64_t units = rows < most ? rows : most;
     p.per_unit = (int)((rows + units - 1) / units);
     p.units = (int)((rows + p.per_unit - 1) / p.per_unit);
     return p;
 }
 
-template <typename T, bool BACKWARD>
-int launch(const Plan& p, const NormArgs& a, cudaStream_t s) {
+template <typename T, bool VEC, bool BACKWARD>
+int launch_as(const Plan& p, const NormArgs& a, cudaStream_t s) {
     const unsigned grid = (unsigned)(p.G == 32 ? (p.units + 7) / 8 : p.units);
     auto go = [&](auto kernel, int threads) { return (int)rtoss_dev::launch_pdl(kernel, grid, (unsigned)threads, 0, s, a); };
     if (p.P == 0) return go(norm_long_kernel<T, BACKWARD>, kLongThreads);
     if (BACKWARD) {
-        if (p.G == 32) return go(norm_backward_kernel<T, 32, 1>, 256);
-        if (p.G == 128) return go(norm_backward_kernel<T, 128, 1>, 128);
-        if (p.G == 256) return go(norm_backward_kernel<T, 256, 1>, 256);
-        if (p.P == 1) return go(norm_backward_kernel<T, 512, 1>, 512);
-        return go(norm_backward_kernel<T, 512, 2>, 512);
+        if (p.G == 32) return go(norm_backward_kernel<T, VEC, 32, 1>, 256);
+        if (p.G == 128) return go(norm_backward_kernel<T, VEC, 128, 1>, 128);
+        if (p.G == 256) return go(norm_backward_kernel<T, VEC, 256, 1>, 256);
+        if (p.P == 1) return go(norm_backward_kernel<T, VEC, 512, 1>, 512);
+        return go(norm_backward_kernel<T, VEC, 512, 2>, 512);
     }
-    if (p.G == 32) return go(norm_forward_kernel<T, 32, 1>, 256);
-    if (p.G == 128) return go(norm_forward_kernel<T, 128, 1>, 128);
-    if (p.G == 256) return go(norm_forward_kernel<T, 256, 1>, 256);
-    if (p.P == 1) return go(norm_forward_kernel<T, 512, 1>, 512);
-    return go(norm_forward_kernel<T, 512, 2>, 512);
+    if (p.G == 32) return go(norm_forward_kernel<T, VEC, 32, 1>, 256);
+    if (p.G == 128) return go(norm_forward_kernel<T, VEC, 128, 1>, 128);
+    if (p.G == 256) return go(norm_forward_kernel<T, VEC, 256, 1>, 256);
+    if (p.P == 1) return go(norm_forward_kernel<T, VEC, 512, 1>, 512);
+    return go(norm_forward_kernel<T, VEC, 512, 2>, 512);
+}
+
+template <typename T, bool BACKWARD>
+int launch(const Plan& p, const NormArgs& a, cudaStream_t s) {
+    return a.vec ? launch_as<T, true, BACKWARD>(p, a, s) : launch_as<T, false, BACKWARD>(p, a, s);
 }
 
 bool norm_ok(int k) { return k == RTOSS_NORM_NONE || k == RTOSS_NORM_RMS || k == RTOSS_NORM_LAYER; }
@@ -601,8 +636,9 @@ int backward(const rtoss_block_norm* b, const Plan& p, cudaStream_t s) {
     if (const int e = launch<T, true>(p, a, s)) return e;
     const bool join_gates = a.dgate && p.units > 1 && p.per_unit % a.S != 0;   // (else every gate's rows were one unit's)
     if (!a.p_post && !a.p_pre && !join_gates) return 0;
-    JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.units, p.per_unit, a.S};
-    return (int)rtoss_dev::launch_pdl(norm_join_kernel<T>, dim3((unsigned)((b->D + 31) / 32), (unsigned)(2 + (join_gates ? p.units - 1 : 0))), dim3(256), 0, s, j);
+    const int gates = (int)(b->tokens / a.S), by_gate = gates < p.units;
+    JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.units, p.per_unit, a.S, by_gate};
+    return (int)rtoss_dev::launch_pdl(norm_join_kernel<T>, dim3((unsigned)((b->D + 31) / 32), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.units - 1))), dim3(kJoinRuns * 32), 0, s, j);
 }
 
 }  // namespace
@@ -614,14 +650,14 @@ rtoss_status rtoss_block_norm_forward(rtoss_ctx* ctx, const rtoss_block_norm* b,
     if (st != RTOSS_OK || b->tokens == 0) return st;
     rtoss_device_guard on_device(ctx->device);
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    const Plan p = plan_of(b->tokens, b->D, ctx->sm_count > 0 ? ctx->sm_count : 148);
+    const Plan p = plan_of(b->tokens, b->D, ctx->sm_count > 0 ? ctx->sm_count : 148, false);
     const NormArgs a = args_of(b, p, false);
     return launched(ctx, kFwd, b->dtype == RTOSS_F32 ? launch<float, false>(p, a, s) : b->dtype == RTOSS_BF16 ? launch<__nv_bfloat16, false>(p, a, s) : launch<__half, false>(p, a, s));
 }
 
 rtoss_status rtoss_block_norm_workspace(const rtoss_ctx* ctx, int64_t tokens, int D, int gated, int64_t* floats) {
     if (!ctx || !floats || tokens < 0 || D < 1 || tokens > kMaxDim || D > kMaxDim) return RTOSS_ERR_INVALID_ARG;
-    *floats = tokens ? ws_floats(plan_of(tokens, D, ctx->sm_count > 0 ? ctx->sm_count : 148), D, gated != 0) : 0;
+    *floats = tokens ? ws_floats(plan_of(tokens, D, ctx->sm_count > 0 ? ctx->sm_count : 148, true), D, gated != 0) : 0;
     return RTOSS_OK;
 }
 
@@ -635,7 +671,7 @@ rtoss_status rtoss_block_norm_backward(rtoss_ctx* ctx, const rtoss_block_norm* b
         if (!e && b->dpre_weight_dev) e = (int)cudaMemsetAsync(b->dpre_weight_dev, 0, sizeof(float) * (size_t)b->D, s);
         return launched(ctx, kBwd, e);
     }
-    const Plan p = plan_of(b->tokens, b->D, ctx->sm_count > 0 ? ctx->sm_count : 148);
+    const Plan p = plan_of(b->tokens, b->D, ctx->sm_count > 0 ? ctx->sm_count : 148, true);
     if (b->dpost_weight_dev || b->dpre_weight_dev || b->dgate.dev) {
         if (!b->workspace_dev) return fail(ctx, RTOSS_ERR_INVALID_ARG, kBwd, "null workspace");
         if (!aligned16(b->workspace_dev)) return fail(ctx, RTOSS_ERR_ALIGNMENT, kBwd, "the workspace must be 16-byte aligned");
