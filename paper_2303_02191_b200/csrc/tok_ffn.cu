@@ -59,7 +59,7 @@ rtoss_status check(rtoss_ctx* ctx, const rtoss_ffn* f, bool backward, const char
 
 template <typename T, int MODE, int NP>
 int run_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np, bool a_mn, bool b_mn, cudaStream_t s) {
-    const Shape c = choose_shape(ps, np, MODE == kGated, MODE == kGateGrad, 64, ctx->sm_count > 0 ? ctx->sm_count : 148);
+    const Shape c = choose_shape(ps, np, MODE == kGated, 64, ctx->sm_count > 0 ? ctx->sm_count : 148);
     return c.bn == 256 ? launch_gemm<T, MODE, 256, NP>(ctx, g, ps, np, a_mn, b_mn, c.KS, s) : launch_gemm<T, MODE, 128, NP>(ctx, g, ps, np, a_mn, b_mn, c.KS, s);
 }
 
@@ -98,8 +98,7 @@ int backward(const rtoss_ctx* ctx, const rtoss_ffn* f, cudaStream_t s) {
                dx = rows_of(f->dx, f->D), dwg = rows_of(f->dw_gate, f->D), dwu = rows_of(f->dw_up, f->D), dwd = rows_of(f->dw_down, f->F);
     GemmArgs<1> g = {};
     g.act = f->act;
-    g.e0 = gate.p, g.e_ld = gate.ld, g.e1 = up.p, g.e1_ld = up.ld;
-    const Product grad = {M, f->F, f->D, 1, {dy, dy}, {wd, wd}, {h, dg, du}};
+    const Product grad = {M, f->F, f->D, 1, {dy, dy}, {wd, wd}, {h, dg, du}, {gate, up}};
     if (const int e = run_gemm<T, kGateGrad, 1>(ctx, g, &grad, 1, false, true, s)) return e;
     if (dx.p) {
         GemmArgs<3> d = {};
@@ -149,3 +148,4 @@ rtoss_status rtoss_gated_ffn_backward(rtoss_ctx* ctx, const rtoss_ffn* f, void* 
 }
 
 }  // extern "C"
+

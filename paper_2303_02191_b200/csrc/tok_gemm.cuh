@@ -46,7 +46,7 @@ constexpr int kEpiWarps = 8;
 constexpr int kMaxKS = 4;   // shares of k: clusters of at most 8 CTAs
 
 struct GemmProblem {
-    CUtensorMap a[2], b[2], o[3];   // operands by k segment (kGated: b by half), outputs
+    CUtensorMap a[2], b[2], o[3];   // operands by k segment (kGated: b by half), outputs (kPlain: o[1] has boxes of 32 columns)
     void* op[3];                    // the outputs again, for columns that a TMA store cannot cut off
     long long o_ld[3];
     int M, N;                       // rows and columns of the output
@@ -64,10 +64,9 @@ struct GemmArgs {
     int save;                       // kGated: gate and up are written too
     int* status;
     long long wait;
-    // kGateGrad: the saved projections; kInt8: scales, bias, residual
-    const void* e0;
-    const void* e1;
-    long long e_ld, e1_ld;
+    CUtensorMap e[2];               // kGateGrad: the saved projections
+    const void* res;                // kInt8: residual, scales, bias
+    long long res_ld;
     const float* row_scale;
     const float* col_scale;
     const float* bias;
@@ -85,14 +84,19 @@ struct GemmShape {
     static constexpr int kUnits = BN / kUnitAcc;
     static constexpr int kOutRow = kUnitCols * (int)sizeof(T);                     // bytes of a staged output row: 64 or 128
     static constexpr int kOuts = MODE == kGated || MODE == kGateGrad ? 3 : 1;
-    static constexpr int kStagingBytes = kOutRow * 32 * kOuts + (MODE == kInt8 ? 1024 : 0);                     // of a warp
+    static constexpr int kPatch = kOutRow * 32;                                    // bytes of a warp's unit of one output
+    static constexpr int kSet = kPatch * kOuts;
+    // kGateGrad: two sets, whose patches take the saved projections before their gradients; kInt8: column scales and biases
+    static constexpr int kStagingBytes = MODE == kGateGrad ? 2 * kSet : kSet + (MODE == kInt8 ? 1024 : 0);
+    // columns of accumulators that the CTAs of a split tile deal out, and what they make of the output
+    static constexpr int kShareAcc = MODE == kGated ? 64 : 32, kShares = BN / kShareAcc;                     // of a warp
     static constexpr int kRoom = 226 * 1024 - kEpiWarps * kStagingBytes;
     static constexpr int kStages = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
-    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 256;
+    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 512;
     static constexpr int kTileN = MODE == kGated ? BN / 2 : BN;                    // output columns of a tile
     static constexpr int kTmemCols = 2 * BN;
     // the exchange of a split tile lies in the operand ring
-    static_assert(kUnits * 4 * 32 * kUnitAcc * 4 <= kStages * kStageBytes, "no room for the exchange");
+    static_assert(BN * 128 * 4 <= kStages * kStageBytes, "no room for the exchange");
     static_assert(kSmem <= 227 * 1024, "shared memory");
     static_assert(kTmemCols <= 512, "TMEM");
 };
@@ -146,6 +150,12 @@ __device__ __forceinline__ void load_box(unsigned dst, const CUtensorMap* map, i
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
+}
+// (a barrier of this CTA)
+__device__ __forceinline__ void load_own(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
 }
 __device__ __forceinline__ void store_box(const CUtensorMap* map, int x, int y, unsigned src) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
@@ -265,6 +275,10 @@ __device__ __forceinline__ void unstage_row(unsigned patch, int lane, void* base
     }
 }
 
+__device__ __forceinline__ uint4 staged_piece(unsigned patch, int lane, int j) {
+    return ld_shared16(patch + (unsigned)(lane * 64) + (((unsigned)j ^ (unsigned)((lane >> 1) & 3)) << 4));
+}
+
 // 32 consecutive values of one row of a [rows, cols] operand of the epilogue (zeros outside; no byte behind the row's last
 // value is read).
 template <typename T>
@@ -304,7 +318,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
     extern __shared__ unsigned char smem_raw[];
     const unsigned raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const unsigned s_stage = base, s_out = base + S::kStages * S::kStageBytes, s_bar = s_out + kEpiWarps * S::kStagingBytes;
-    const unsigned b_full = s_bar, b_empty = s_bar + 64, b_acc_full = s_bar + 128, b_acc_empty = s_bar + 144, s_tmem = s_bar + 160;
+    const unsigned b_full = s_bar, b_empty = s_bar + 64, b_acc_full = s_bar + 128, b_acc_empty = s_bar + 144, s_tmem = s_bar + 160, b_edge = s_bar + 176;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const unsigned rank = cta_rank(), half = rank & 1u, lead_rank = rank & ~1u, share = rank >> 1;
     const int KS = g.KS;
@@ -324,6 +338,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             bar_init(b_acc_full + 8 * i, 1);
             bar_init(b_acc_empty + 8 * i, 2 * kEpiWarps);
         }
+        if (MODE == kGateGrad)
+            for (int i = 0; i < 2 * kEpiWarps; ++i) bar_init(b_edge + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -440,52 +456,60 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
 
     // ---- epilogue ---------------------------------------------------------------------------------------------------
     const int quad = warp & 3, side = (warp - 4) >> 2;   // 32 accumulator rows; every other unit of columns
-    const unsigned patch = s_out + (unsigned)((warp - 4) * S::kStagingBytes);
-    auto acc_cols = [&](int u, int j) { return MODE == kGated ? j * (BN / 2) + u * 32 : u * S::kUnitAcc + j * 32; };
-    auto read_unit = [&](int as, int u, unsigned* acc) {
-        const unsigned d = tmem + (unsigned)(as * BN) + ((unsigned)(quad * 32) << 16);
-#pragma unroll
-        for (int j = 0; j < S::kUnitAcc / 32; ++j) tmem_ld32(d + (unsigned)acc_cols(u, j), acc + 32 * j);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    const unsigned staging = s_out + (unsigned)((warp - 4) * S::kStagingBytes);
+    auto read_acc = [&](unsigned at, int cols, unsigned* acc) {   // (not complete before tcgen05.wait::ld)
+        tmem_ld32(at, acc);
+        if (cols == 64) tmem_ld32(at + (MODE == kGated ? BN / 2 : 32), acc + 32);
     };
-    // what a unit needs besides its sums
-    auto fetch = [&](const Tile& at, int u, uint4* e) {
-        const int row = at.mt * 256 + (int)half * 128 + quad * 32 + lane, col = at.nt * S::kTileN + u * S::kUnitCols;
-        if constexpr (MODE == kGateGrad) {
-            fetch32<T>(g.e0, g.e_ld, row, at.p->M, col, at.p->N, e);
-            fetch32<T>(g.e1, g.e1_ld, row, at.p->M, col, at.p->N, e + 4);
-        }
+    auto acc_at = [&](int as, int u, int cols) { return tmem + (unsigned)(as * BN + u * (MODE == kGated ? 32 : cols)) + ((unsigned)(quad * 32) << 16); };
+    auto loaded = [] { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); };
+    auto row0_of = [&](const Tile& at) { return at.mt * 256 + (int)half * 128 + quad * 32; };
+    // kInt8: 32 values of the residual; the scale of this lane's row; the scale and bias of the unit's column `lane`
+    auto residual_of = [&](const Tile& at, int col, uint4* e) {
         if constexpr (MODE == kInt8) {
-            if (g.e0) fetch32<T>(g.e0, g.e_ld, row, at.p->M, col, at.p->N, e);
+            if (g.res) fetch32<T>(g.res, g.res_ld, row0_of(at) + lane, at.p->M, col, at.p->N, e);
         }
     };
-    // kInt8: the scale of this lane's row, and the scale and bias of the unit's column `lane`
-    auto row_of = [&](const Tile& at) {
-        const int row = at.mt * 256 + (int)half * 128 + quad * 32 + lane;
-        return MODE == kInt8 && row < at.p->M ? g.row_scale[row] : 0.f;
-    };
-    auto column_of = [&](const Tile& at, int u) {
+    auto row_scale_of = [&](const Tile& at) { return MODE == kInt8 && row0_of(at) + lane < at.p->M ? g.row_scale[row0_of(at) + lane] : 0.f; };
+    auto column_of = [&](const Tile& at, int col) {
         float2 cb = make_float2(0.f, 0.f);
-        const int col = at.nt * S::kTileN + u * S::kUnitCols + lane;
-        if (MODE == kInt8 && col < at.p->N) {
-            cb.x = g.col_scale[col];
-            if (g.bias) cb.y = g.bias[col];
+        if (MODE == kInt8 && col + lane < at.p->N) {
+            cb.x = g.col_scale[col + lane];
+            if (g.bias) cb.y = g.bias[col + lane];
         }
         return cb;
     };
-    auto finish = [&](const Tile& at, int u, unsigned* acc, const uint4* e, float row_scale, float2 cb) {
+    // kGateGrad: the saved projections of a unit (the asked-th of this warp) on their way into the patches of a set, which the
+    // unit before the last one has left.
+    unsigned asked = 0, taken = 0;
+    auto ask = [&](const Tile& at, int col) {
+        if constexpr (MODE == kGateGrad) {
+            const int row0 = row0_of(at);
+            if (row0 >= at.p->M || col >= at.p->N) return;
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                const unsigned set = staging + (asked & 1u) * S::kSet, bar = b_edge + (unsigned)(16 * (warp - 4)) + 8u * (asked & 1u);
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(2 * S::kPatch) : "memory");
+                load_own(set + S::kPatch, &g.e[0], col, row0, bar);
+                load_own(set + 2 * S::kPatch, &g.e[1], col, row0, bar);
+            }
+            ++asked;
+        }
+    };
+    // A unit's sums to its outputs.  COLS: columns of the unit's outputs (32, or 64 in kPlain).  false: a wait ran out.
+    auto finish = [&](const Tile& at, int col, auto cols_c, unsigned* acc, const uint4* e, float row_scale, float2 cb) {
+        constexpr int COLS = decltype(cols_c)::value;
         const GemmProblem& p = *at.p;
-        const int row0 = at.mt * 256 + (int)half * 128 + quad * 32, col = at.nt * S::kTileN + u * S::kUnitCols;
-        if (row0 >= p.M || col >= p.N) return;   // (the same for all lanes)
+        const int row0 = row0_of(at);
+        if (row0 >= p.M || col >= p.N) return true;   // (the same for all lanes)
         float* v = reinterpret_cast<float*>(acc);
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the patch is free
-        __syncwarp();
+        unsigned patch = staging;
         if constexpr (MODE == kPlain) {
-            stage_row<T, 64>(patch, lane, v);
+            stage_row<T, COLS>(patch, lane, v);
         } else if constexpr (MODE == kGated) {
             if (g.save) {
-                stage_row<T, 32>(patch + S::kOutRow * 32, lane, v);
-                stage_row<T, 32>(patch + 2 * S::kOutRow * 32, lane, v + 32);
+                stage_row<T, 32>(patch + S::kPatch, lane, v);
+                stage_row<T, 32>(patch + 2 * S::kPatch, lane, v + 32);
             }
             with_act(g.act, [&](auto act) {
 #pragma unroll
@@ -493,27 +517,31 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             });
             stage_row<T, 32>(patch, lane, v);
         } else if constexpr (MODE == kGateGrad) {
+            patch = staging + (taken & 1u) * S::kSet;
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(b_edge + (unsigned)(16 * (warp - 4)) + 8u * (taken & 1u), (taken >> 1) & 1u, g.wait))) return false;
+            ++taken;
             with_act(g.act, [&](auto act) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {   // a 16-byte piece of each output at a time
+                for (int j = 0; j < 4; ++j) {   // a 16-byte piece of each at a time; the gradients take the projections' places
+                    const uint4 gw = staged_piece(patch + S::kPatch, lane, j), uw = staged_piece(patch + 2 * S::kPatch, lane, j);
                     float h[8], dg[8], du[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float gv = value_of<T>(e, j + i), uv = value_of<T>(e + 4, j + i);
+                        const float gv = value_of<T>(&gw, i), uv = value_of<T>(&uw, i), dh = v[8 * j + i];
                         float slope;
                         const float a = act_slope<decltype(act)::value>(gv, &slope);
-                        dg[i] = v[j + i] * uv * slope;
-                        du[i] = v[j + i] * a;
+                        dg[i] = dh * uv * slope;
+                        du[i] = dh * a;
                         h[i] = a * uv;
                     }
-                    stage_piece<T>(patch, lane, j / 8, h);
-                    stage_piece<T>(patch + S::kOutRow * 32, lane, j / 8, dg);
-                    stage_piece<T>(patch + 2 * S::kOutRow * 32, lane, j / 8, du);
+                    stage_piece<T>(patch, lane, j, h);
+                    stage_piece<T>(patch + S::kPatch, lane, j, dg);
+                    stage_piece<T>(patch + 2 * S::kPatch, lane, j, du);
                 }
             });
         } else {
             // the unit's column scales and biases: a lane fetches one of each, all lanes read all
-            const unsigned cols_at = patch + S::kOutRow * 32;
+            const unsigned cols_at = patch + S::kPatch;
             __syncwarp();
             asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(cols_at + 8u * (unsigned)lane), "f"(cb.x), "f"(cb.y) : "memory");
             __syncwarp();
@@ -521,62 +549,85 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
 #pragma unroll
                 for (int j = 0; j < 32; j += 2) {
                     const uint4 w = ld_shared16(cols_at + 8u * j);
-                    const float r0 = g.e0 ? value_of<T>(e, j) : 0.f, r1 = g.e0 ? value_of<T>(e, j + 1) : 0.f;
+                    const float r0 = g.res ? value_of<T>(e, j) : 0.f, r1 = g.res ? value_of<T>(e, j + 1) : 0.f;
                     v[j] = i8_value<decltype(act)::value>((int)acc[j], row_scale, __uint_as_float(w.x), __uint_as_float(w.y), r0, g.res_after);
                     v[j + 1] = i8_value<decltype(act)::value>((int)acc[j + 1], row_scale, __uint_as_float(w.z), __uint_as_float(w.w), r1, g.res_after);
                 }
             });
             stage_row<T, 32>(patch, lane, v);
         }
-        if (col + S::kUnitCols > p.N && p.N % (16 / (int)sizeof(T)) != 0) {
+        if (col + COLS > p.N && p.N % (16 / (int)sizeof(T)) != 0) {
             __syncwarp();
-            unstage_row<T, S::kUnitCols>(patch, lane, p.op[0], p.o_ld[0], row0 + lane, p.M, col, p.N);
+            unstage_row<T, COLS>(patch, lane, p.op[0], p.o_ld[0], row0 + lane, p.M, col, p.N);
             if ((MODE == kGated && g.save) || MODE == kGateGrad) {
-                unstage_row<T, S::kUnitCols>(patch + S::kOutRow * 32, lane, p.op[1], p.o_ld[1], row0 + lane, p.M, col, p.N);
-                unstage_row<T, S::kUnitCols>(patch + 2 * S::kOutRow * 32, lane, p.op[2], p.o_ld[2], row0 + lane, p.M, col, p.N);
+                unstage_row<T, COLS>(patch + S::kPatch, lane, p.op[1], p.o_ld[1], row0 + lane, p.M, col, p.N);
+                unstage_row<T, COLS>(patch + 2 * S::kPatch, lane, p.op[2], p.o_ld[2], row0 + lane, p.M, col, p.N);
             }
-            return;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            return true;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
-            store_box(&p.o[0], col, row0, patch);
+            store_box(&p.o[MODE == kPlain && COLS == 32 ? 1 : 0], col, row0, patch);
             if ((MODE == kGated && g.save) || MODE == kGateGrad) {
-                store_box(&p.o[1], col, row0, patch + S::kOutRow * 32);
-                store_box(&p.o[2], col, row0, patch + 2 * S::kOutRow * 32);
+                store_box(&p.o[1], col, row0, patch + S::kPatch);
+                store_box(&p.o[2], col, row0, patch + 2 * S::kPatch);
             }
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
+        return true;
+    };
+    auto patch_free = [&] {   // (kGateGrad: ask() has seen to it)
+        if (MODE == kGateGrad) return;
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
     };
 
     bool ok = true;
     if (warp >= 4 && KS == 1) {
         int as = 0;
         unsigned aph = 0;
-        for (int t = cluster; t < g.tiles; t += clusters) {
+        if (cluster < g.tiles) {
+            const Tile at = tile_of(cluster);
+            ask(at, at.nt * S::kTileN + side * S::kUnitCols);
+        }
+        for (int t = cluster; t < g.tiles && ok; t += clusters) {
             const Tile at = tile_of(t);
+            const int col0 = at.nt * S::kTileN;
             uint4 e[8], e_next[8];
-            fetch(at, side, e);
-            const float rs = row_of(at);
-            float2 cb = column_of(at, side), cb_next = cb;
+            residual_of(at, col0 + side * S::kUnitCols, e);
+            const float rs = row_scale_of(at);
+            float2 cb = column_of(at, col0 + side * S::kUnitCols), cb_next = cb;
             if (!(ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full + 8 * as, aph, g.wait)))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int u = side; u < S::kUnits; u += 2) {
                 unsigned acc[S::kUnitAcc];
-                read_unit(as, u, acc);
+                read_acc(acc_at(as, u, S::kUnitAcc), S::kUnitAcc, acc);
+                const int next = col0 + (u + 2) * S::kUnitCols;
                 if (u + 2 < S::kUnits) {
-                    fetch(at, u + 2, e_next);
-                    cb_next = column_of(at, u + 2);
-                } else {   // all sums of this tile are in registers: the pair may overwrite them
+                    ask(at, next);
+                    residual_of(at, next, e_next);
+                    cb_next = column_of(at, next);
+                } else if (MODE == kGateGrad && t + clusters < g.tiles) {
+                    const Tile then = tile_of(t + clusters);
+                    ask(then, then.nt * S::kTileN + side * S::kUnitCols);
+                }
+                patch_free();
+                loaded();
+                if (u + 2 >= S::kUnits) {
+                    // All sums of this tile are in registers: the pair may overwrite them.  Nothing else is handed over, and a release
+                    // would wait for the stores on their way, 3000 clocks.
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0)
-                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(b_acc_empty + 8 * as, lead_rank)) : "memory");
+                        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(b_acc_empty + 8 * as, lead_rank)) : "memory");
                 }
-                finish(at, u, acc, e, rs, cb);
+                ok = finish(at, col0 + u * S::kUnitCols, std::integral_constant<int, S::kUnitCols>(), acc, e, rs, cb) && ok;
                 cb = cb_next;
-                if constexpr (MODE == kGateGrad || MODE == kInt8) {
+                if constexpr (MODE == kInt8) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) e[j] = e_next[j];
                 }
@@ -587,7 +638,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
     }
     if (KS > 1) {
         // One tile a cluster.  Behind the first barrier every pair's products are complete, so the operand rings are free and
-        // take the other pairs' sums: unit u belongs to the pair u * KS / kUnits.
+        // take the other pairs' sums: of the tile's kShares pieces, the next kShares / KS belong to each pair.
         const Tile at = tile_of(cluster);
         if (warp >= 4) {
             ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full, 0, g.wait));
@@ -595,51 +646,69 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
         }
         __syncthreads();
         cluster_barrier();
-        constexpr unsigned kSlot = 32 * S::kUnitAcc * 4;   // a warp's sums of a unit
-        const int per = S::kUnits / KS;
+        constexpr int kAcc = S::kShareAcc;
+        constexpr unsigned kSlot = 32 * kAcc * 4;   // a warp's sums of a piece
+        const int per = S::kShares / KS;
         auto slot = [&](int u, unsigned from) { return s_stage + ((unsigned)((u % per) * KS + (int)from) * 4u + (unsigned)quad) * kSlot + (unsigned)lane * 16u; };
         if (warp >= 4 && ok) {
 #pragma unroll 1
-            for (int u = side; u < S::kUnits; u += 2) {
+            for (int u = side; u < S::kShares; u += 2) {
                 const unsigned owner = (unsigned)(u / per);
                 if (owner == share) continue;
-                unsigned acc[S::kUnitAcc];
-                read_unit(0, u, acc);
+                unsigned acc[kAcc];
+                read_acc(acc_at(0, u, kAcc), kAcc, acc);
+                loaded();
                 const unsigned to = at_rank(slot(u, share), 2 * owner + half);
 #pragma unroll
-                for (int j = 0; j < S::kUnitAcc / 4; ++j) st_cluster16(to + j * 512, acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+                for (int j = 0; j < kAcc / 4; ++j) st_cluster16(to + j * 512, acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
             }
         }
         __syncthreads();
         cluster_barrier();
         if (warp >= 4 && ok) {
 #pragma unroll 1
-            for (int u = (int)share * per; u < ((int)share + 1) * per; ++u) {
-                if ((u & 1) != side && per > 1) continue;
-                if (per == 1 && side != 0) continue;
+            for (int u = (int)share * per + (per > 1 ? side : 0); u < ((int)share + 1) * per; u += per > 1 ? 2 : 1) {
+                if (per == 1 && side != 0) break;
+                const int col = at.nt * S::kTileN + u * 32;
                 uint4 e[8];
-                fetch(at, u, e);
-                unsigned acc[S::kUnitAcc];
-                read_unit(0, u, acc);
+                ask(at, col);
+                residual_of(at, col, e);
+                const float rs = row_scale_of(at);
+                const float2 cb = column_of(at, col);
+                unsigned sum[kAcc];
                 // shares are added in their order, whichever pair adds them
-                unsigned sum[S::kUnitAcc];
 #pragma unroll
-                for (int j = 0; j < S::kUnitAcc; ++j) sum[j] = 0u;
+                for (int j = 0; j < kAcc; ++j) sum[j] = 0u;
+                auto add = [&](int j, unsigned w) {
+                    if constexpr (MODE == kInt8) sum[j] += w;
+                    else sum[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(w));
+                };
 #pragma unroll 1
                 for (unsigned from = 0; from < (unsigned)KS; ++from) {
+                    if (from == share) {
+                        unsigned acc[kAcc];
+                        read_acc(acc_at(0, u, kAcc), kAcc, acc);
+                        loaded();
 #pragma unroll
-                    for (int j = 0; j < S::kUnitAcc / 4; ++j) {
-                        uint4 w = make_uint4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
-                        if (from != share) w = ld_shared16(slot(u, from) + j * 512);
-                        const unsigned* we = reinterpret_cast<const unsigned*>(&w);
+                        for (int j = 0; j < kAcc; ++j) add(j, acc[j]);
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if constexpr (MODE == kInt8) sum[4 * j + i] += we[i];
-                            else sum[4 * j + i] = __float_as_uint(__uint_as_float(sum[4 * j + i]) + __uint_as_float(we[i]));
+                        for (int h = 0; h < kAcc; h += 32) {   // eight loads in flight
+                            uint4 w[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) w[j] = ld_shared16(slot(u, from) + (h / 4 + j) * 512);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                add(h + 4 * j, w[j].x);
+                                add(h + 4 * j + 1, w[j].y);
+                                add(h + 4 * j + 2, w[j].z);
+                                add(h + 4 * j + 3, w[j].w);
+                            }
                         }
                     }
                 }
-                finish(at, u, sum, e, row_of(at), column_of(at, u));
+                patch_free();
+                ok = finish(at, col, std::integral_constant<int, 32>(), sum, e, rs, cb) && ok;
             }
         }
     }

@@ -18,6 +18,7 @@ struct Product {
     int segments;
     Rows a[2], b[2];    // kGated: b[0] the gate's weights, b[1] the up projection's (N: columns of h)
     Rows out[3];
+    Rows edge[2];       // kGateGrad: the saved projections
 };
 
 template <typename T> struct MapType;
@@ -47,16 +48,17 @@ int resident_clusters(Kernel kernel, int smem, int cluster, int sms) {
 }
 
 // Shape of a launch.  Clocks of a block of 128 bytes of k: 4 instructions of 128 clocks (256 columns) or, bound by what shared
-// memory moves, about 4 x 100 (128 columns).  Shares of k cost the exchange, about 3000 clocks.
+// memory moves, about 4 x 100 (128 columns).  Shares of k cost the exchange: two barriers of the cluster and reading the sums, about
+// 4000 clocks, and what a CTA sends at 24 bytes a clock (traced).
 struct Shape {
     int bn, KS;
     double clocks;
 };
-inline Shape choose_shape(const Product* ps, int np, bool gated, bool narrow_units, int kper, int sms) {
+inline Shape choose_shape(const Product* ps, int np, bool gated, int kper, int sms) {
     const int pairs = sms / 2;
     Shape best = {256, 1, 1e300};
     for (int bn = 256; bn >= 128; bn -= 128) {
-        const int tn = gated ? bn / 2 : bn, units = bn / (narrow_units ? 32 : 64);
+        const int tn = gated ? bn / 2 : bn, shares = bn / (gated ? 64 : 32);
         int64_t tiles = 0;
         int kb = 0, kb_min = 1 << 30;
         double work = 0;
@@ -69,11 +71,11 @@ inline Shape choose_shape(const Product* ps, int np, bool gated, bool narrow_uni
             kb_min = k < kb_min ? k : kb_min;
         }
         const double per_kb = bn == 256 ? 512.0 : 400.0;
-        for (int ks = 1; ks <= kMaxKS && ks <= units; ks *= 2) {
+        for (int ks = 1; ks <= kMaxKS && ks <= shares; ks *= 2) {
             if (ks > 1 && (np > 1 || kb_min < 4 * ks || tiles * ks > pairs)) continue;
             const double waves = (double)((tiles * ks + pairs - 1) / pairs);
             const double c = ks == 1 ? (waves < 4 ? waves * kb * per_kb : work / pairs * per_kb) + 2000.0
-                                     : (double)((kb + ks - 1) / ks) * per_kb + 5000.0;
+                                     : (double)((kb + ks - 1) / ks) * per_kb + 6000.0 + 512.0 * bn * (ks - 1) / ks / 24.0;
             if (c < best.clocks) best = {bn, ks, c};
         }
     }
@@ -136,10 +138,14 @@ int launch_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np
             const Rows& out = p.out[o].p ? p.out[o] : p.out[0];
             q.op[o] = const_cast<void*>(out.p);
             q.o_ld[o] = out.ld;
-            if (o && !p.out[o].p) q.o[o] = q.o[0];
+            if (MODE == kPlain && o == 1) ok = ok && encode_rows(&q.o[1], MapType<T>::v, out.p, p.M, p.N, out.ld * (int64_t)sizeof(T), 32, 32, 64);
+            else if (o && !p.out[o].p) q.o[o] = q.o[0];
             else ok = ok && encode_rows(&q.o[o], MapType<T>::v, out.p, p.M, p.N, out.ld * (int64_t)sizeof(T), S::kUnitCols, 32, S::kOutRow);
         }
     }
+    if constexpr (MODE == kGateGrad)
+        for (int o = 0; o < 2; ++o)
+            ok = ok && encode_rows(&g.e[o], MapType<T>::v, ps[0].edge[o].p, ps[0].M, ps[0].N, ps[0].edge[o].ld * (int64_t)sizeof(T), 32, 32, 64);
     if (!ok) return (int)cudaErrorInvalidValue;
     if (tiles > 0x3FFFFFFF) return (int)cudaErrorInvalidConfiguration;
     g.tiles = (int)tiles;

@@ -16,8 +16,15 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
     else f(std::integral_constant<int, RTOSS_ACT_NONE>());
 }
 
-// 1 / (1 + e^-v): the exponential overflows to infinity below -88, and the quotient is then the 0 it should be.
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// 1 / (1 + e^-v) in the two special-function instructions it takes (2 ulp and 1 ulp).  Flushing subnormals costs nothing here: a
+// subnormal exponential vanishes beside the 1, and below -88, where the exponential overflows, the quotient is the 0 it should
+// be.  (__expf and __fdividef keep subnormals, at twice the time of an epilogue.)
+__device__ __forceinline__ float sigmoid(float v) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
+}
 
 // NaN goes through every activation.
 template <int ACT>
