@@ -7,10 +7,13 @@
 // bound: bytes.  A row is read once and every intermediate stays in registers: forward 4 rows of traffic a token, backward 6
 // (r, y, dz, dn in, dr, dy out).  The backward pass forms v and z again from r and y in fp32: reading the stored z instead would
 // cost the same bytes and bring its rounding into every gradient.  A unit of G threads takes a contiguous run of rows; weights,
-// gates and the sums over tokens stay in its registers, and the next row is on its way while this one is reduced.  Sums over
-// tokens (the gradients of weights and gates) end as one row per unit in the workspace and are added in the units' order by
+// gates and the sums over tokens stay in its registers, and the next rows are on their way while this one is reduced (RowFeed).
+// The arithmetic goes in pairs (fma.rn.f32x2), without which the backward pass would be bound by what an SM issues.  Sums over
+// tokens (the gradients of weights and gates) end as one row per block in the workspace and are added in the blocks' order by
 // a second launch: no atomics, the same bits every time.  All arithmetic is fp32; squares are summed after the mean is
 // subtracted, not as a difference of moments.
+#include <atomic>
+
 #include "tok_internal.h"
 #include "tok_math.cuh"
 
@@ -22,6 +25,7 @@ using rtoss_dev::to_f32;
 
 constexpr const char* kFwd = "block norm forward";
 constexpr const char* kBwd = "block norm backward";
+constexpr int kMaxStages = 6;
 
 struct NormArgs {
     const void *r, *y, *dz, *dn, *gate;
@@ -32,9 +36,31 @@ struct NormArgs {
     int S;             // tokens that share a gate
     int per_unit;      // rows of a unit
     float scale, eps;
-    float *p_post, *p_pre, *p_gate;   // partial sums: [unit][D], [unit][D], [unit][2][D]
+    int stages;        // rows that the ring of a block holds (RowFeed)
+    int* status;
+    long long wait;    // limit of a wait, in clocks
+    float *p_post, *p_pre, *p_gate;   // partial sums: [block][D], [block][D], [unit][2][D]
     void* dgate;
 };
+
+// ---- pairs of values: one instruction for both -------------------------------------------------------------------------
+__device__ __forceinline__ unsigned long long& bits2(float2& v) { return reinterpret_cast<unsigned long long&>(v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)));
+    return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // ---- eight values -----------------------------------------------------------------------------------------------------
 // As they lie in memory: a row's loads stay in flight until its values are widened.
@@ -60,313 +86,527 @@ __device__ __forceinline__ void zero8(Raw<T>& r) {
     for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(&r)[j] = make_uint4(0u, 0u, 0u, 0u);
 }
 template <typename T>
-__device__ __forceinline__ void widen8(const Raw<T>& r, float (&v)[8]) {
+__device__ __forceinline__ void widen8(const Raw<T>& r, float2 (&v)[4]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = to_f32<T>(r.e[j]);
+    for (int j = 0; j < 4; ++j) v[j] = make_float2(to_f32<T>(r.e[2 * j]), to_f32<T>(r.e[2 * j + 1]));
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const void* base, long long ld, int row, int i, int D, float (&v)[8]) {
+__device__ __forceinline__ void load8(const void* base, long long ld, int row, int i, int D, float2 (&v)[4]) {
     Raw<T> r;
     fetch8<T, VEC>(base, ld, row, i, D, r);
     widen8<T>(r, v);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(void* base, long long ld, int row, int i, int D, const float (&v)[8]) {
+__device__ __forceinline__ void store8(void* base, long long ld, int row, int i, int D, const float2 (&v)[4]) {
     T* at = reinterpret_cast<T*>(base) + (long long)row * ld + i;
     if (VEC) {
         Raw<T> r;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.e[j] = from_f32<T>(v[j]);
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) reinterpret_cast<__nv_bfloat162*>(&r)[j] = __floats2bfloat162_rn(v[j].x, v[j].y);
+            else if constexpr (std::is_same<T, __half>::value) reinterpret_cast<__half2*>(&r)[j] = __floats2half2_rn(v[j].x, v[j].y);
+            else reinterpret_cast<float2*>(&r)[j] = v[j];
+        }
 #pragma unroll
         for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(at)[j] = reinterpret_cast<const uint4*>(&r)[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i + j < D) at[j] = from_f32<T>(v[j]);
+        for (int j = 0; j < 4; ++j) {
+            if (i + 2 * j < D) at[2 * j] = from_f32<T>(v[j].x);
+            if (i + 2 * j + 1 < D) at[2 * j + 1] = from_f32<T>(v[j].y);
+        }
     }
 }
 
-// Sums of N values over the G threads of a unit (G = 32: a warp of its own).  Consecutive calls take alternating halves of the
-// buffer, so that one barrier a call is enough.
+// Sums of N <= 3 values over the G threads of a unit, in a fixed order.  Up to 32 they are part of a warp; else several values
+// share the shuffles (at each of the first steps a lane hands half of what it holds to the lane across and keeps the other
+// half) and the warps meet in shared memory, where the places of warps that the block does without hold zeros.  Consecutive
+// calls take alternating halves of the buffer, so that one barrier a call is enough.
 template <int G>
 struct Reduce {
-    float* buf;   // [2][2][G / 32]
+    static constexpr int W = G <= 32 ? 1 : G / 32;
+    static constexpr int kFloats = G <= 32 ? 4 : 2 * 4 * W;
+    float* buf;   // [2][4][W], 16-byte aligned
     int turn, warp, lane;
+    // (all threads of the block; a barrier has to follow)
+    __device__ __forceinline__ void clear() {
+        if (G > 32)
+            for (int i = (int)threadIdx.x; i < kFloats; i += (int)blockDim.x) buf[i] = 0.f;
+    }
     template <int N>
     __device__ __forceinline__ void sum(float (&v)[N]) {
+        if constexpr (G <= 32) {
 #pragma unroll
-        for (int k = 0; k < N; ++k)
+            for (int k = 0; k < N; ++k)
 #pragma unroll
-            for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-        if (G > 32) {
-            constexpr int W = G / 32;
-            float* b = buf + turn * 2 * W;
+                for (int o = G / 2; o; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+        } else {
+            float* b = buf + turn * 4 * W;
             turn ^= 1;
-            if (lane == 0) {
-#pragma unroll
-                for (int k = 0; k < N; ++k) b[k * W + warp] = v[k];
+            float t = v[0];
+            constexpr int o = N == 1 ? 16 : N == 2 ? 8 : 4;   // the steps left to one value
+            int k = 0;
+            if constexpr (N == 2) {
+                const bool up = lane & 16;
+                t = (up ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, up ? v[0] : v[1], 16);
+                k = lane >> 4;
+            } else if constexpr (N == 3) {
+                const bool up = lane & 16, odd = lane & 8;
+                const float a0 = (up ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, up ? v[0] : v[2], 16);
+                const float a1 = (up ? 0.f : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, up ? v[1] : 0.f, 16);
+                t = (odd ? a1 : a0) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a0 : a1, 8);
+                k = lane >> 3;
             }
+#pragma unroll
+            for (int s = o; s; s >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, s);
+            if ((lane & (2 * o - 1)) == 0 && k < N) b[k * W + warp] = t;
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                float t = lane < W ? b[k * W + lane] : 0.f;
+            for (int n = 0; n < N; ++n) {
+                const float2* w = reinterpret_cast<const float2*>(b + n * W);
+                float2 q = w[0];
 #pragma unroll
-                for (int o = W / 2; o; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-                v[k] = __shfl_sync(0xFFFFFFFFu, t, 0);
+                for (int i = 1; i < W / 2; ++i) q = add2(q, w[i]);
+                v[n] = q.x + q.y;
             }
         }
     }
 };
 
-// Mean (layer norm) and 1 / root of the mean square of the P pieces a thread holds; `in`: the piece lies inside the row.
-template <int P, int G>
-__device__ __forceinline__ void stats(Reduce<G>& red, const float (&v)[P][8], const bool (&in)[P], int at, int D, int kind, float eps, float* mean, float* rstd) {
-    float m = 0.f;
-    if (kind == RTOSS_NORM_LAYER) {
-        float s[1] = {0.f};
+// Units of a block: those of up to a warp share a block of 256 threads, larger ones are blocks of up to G threads (as many warps
+// as the row has pieces for).
+template <int G> constexpr int block_of() { return G <= 32 ? 256 : G; }
+// Blocks of G threads that an SM holds: the forward pass has 64 registers a thread, the backward pass, whose sums over tokens
+// stay in them, 128.
+template <int G, int P, bool BACKWARD>
+constexpr int blocks_of() { return (BACKWARD || P == 2 ? 512 : 1024) / block_of<G>(); }
+
+// Rows on their way to a unit, A operands of each.  RING: a block's rows come by bulk copies through a ring of stages in shared
+// memory, up to `stages` rows ahead of the one at work (with one row ahead in registers an SM had 32 KB in flight, too little
+// for 6.5 TB/s: 16384 x 2048 forward took 68 us, with the ring 51).  Otherwise (rows off 16-byte boundaries, and units of up to
+// a warp, whose rows are too short for a copy each) the next row waits in registers.
+template <typename T, bool VEC, int G, int P, int A>
+struct RowFeed {
+    static constexpr bool RING = VEC && G > 32;
+    const void* base[A];
+    long long ld[A];
+    int at, threads, D, row0, row1, stages;
+    // ring
+    unsigned ring, bars, zeros, row_bytes, stage_bytes, tx;
+    int s, s_fill, fill;   // stage of the row at work; stage and row to ask for next
+    unsigned phase;
+    bool dead;
+    long long limit;
+    Raw<T> next[RING ? 1 : A][RING ? 1 : P];
+
+    __device__ __forceinline__ void ask() {   // (thread 0)
+        const unsigned bar = bars + 8u * (unsigned)s_fill, to = ring + (unsigned)s_fill * stage_bytes;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(tx) : "memory");
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[0] += v[p][j];   // (zeros outside the row)
-        red.template sum<1>(s);
-        m = s[0] / (float)D;
+        for (int k = 0; k < A; ++k)
+            if (base[k])
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + (unsigned)k * row_bytes),
+                             "l"(reinterpret_cast<const T*>(base[k]) + (long long)fill * ld[k]), "r"(row_bytes), "r"(bar)
+                             : "memory");
+        ++fill;
+        if (++s_fill == stages) s_fill = 0;
     }
-    float q[1] = {0.f};
+    __device__ __forceinline__ void prefetch(int row) {
+        if constexpr (!RING) {
+#pragma unroll
+            for (int k = 0; k < A; ++k)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    if (base[k] && (p * threads + at) * 8 < D) fetch8<T, VEC>(base[k], ld[k], row, (p * threads + at) * 8, D, next[k][p]);
+        }
+    }
+    // (RING: all threads of the block, before the wait for the kernels in front; a barrier has to follow)
+    __device__ __forceinline__ void prepare() {
+        if constexpr (RING) {
+            if (threadIdx.x == 0) {
+                for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8u * (unsigned)i) : "memory");
+                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            }
+            if (threadIdx.x < 4) asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(zeros + 8u * threadIdx.x), "r"(0) : "memory");
+        }
+    }
+    __device__ __forceinline__ void start() {
+        if constexpr (RING) {
+            s = s_fill = 0, phase = 0, fill = row0, dead = false;
+            row_bytes = (unsigned)D * (unsigned)sizeof(T);
+            stage_bytes = A * row_bytes;
+            tx = 0;
+#pragma unroll
+            for (int k = 0; k < A; ++k) tx += base[k] ? row_bytes : 0u;
+            if (threadIdx.x == 0)
+                for (int i = 0; i < stages && fill < row1; ++i) ask();
+        } else {
+#pragma unroll
+            for (int k = 0; k < A; ++k)
+#pragma unroll
+                for (int p = 0; p < P; ++p) zero8(next[k][p]);
+            if (row0 < row1) prefetch(row0);
+        }
+    }
+    __device__ __forceinline__ unsigned arrived(unsigned bar) const {
+        unsigned done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(phase)
+            : "memory");
+        return done;
+    }
+    // The row's values.  RING: between two calls the block has met at a barrier, so the stage of the row before is free.
+    __device__ __forceinline__ void take(int row, float2 (&v)[A][P][4]) {
+        if constexpr (RING) {
+            if (threadIdx.x == 0 && row > row0 && fill < row1 && !dead) ask();
+            const unsigned bar = bars + 8u * (unsigned)s;
+            if (!arrived(bar) && !dead) {
+                const long long t0 = clock64();
+                while (!arrived(bar))
+                    if (clock64() - t0 > limit) {
+                        dead = true;
+                        break;
+                    }
+            }
+            const unsigned from = ring + (unsigned)s * stage_bytes;
+#pragma unroll
+            for (int k = 0; k < A; ++k)
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    Raw<T> r;
+                    const unsigned i = (unsigned)(p * threads + at) * 8u;
+                    const unsigned a = base[k] && i < (unsigned)D ? from + (unsigned)k * row_bytes + i * (unsigned)sizeof(T) : zeros;
+#pragma unroll
+                    for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+                        uint4& w = reinterpret_cast<uint4*>(&r)[j];
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a + 16u * j) : "memory");
+                    }
+                    widen8<T>(r, v[k][p]);
+                }
+            if (++s == stages) s = 0, phase ^= 1u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < A; ++k)
+#pragma unroll
+                for (int p = 0; p < P; ++p) widen8<T>(next[k][p], v[k][p]);
+            if (row + 1 < row1) prefetch(row + 1);
+        }
+    }
+    // A wait that ran out is told to the host; the copies on their way land before the block ends.
+    __device__ __forceinline__ void finish(int* status) {
+        if constexpr (RING) {
+            if (dead) {
+                atomicExch(status, 4);
+                for (const long long t0 = clock64(); clock64() - t0 < 200000;) {}
+            }
+        }
+    }
+};
+
+// A number, in the places of the thread's piece that lie inside the row (else 0).
+template <bool VEC>
+__device__ __forceinline__ float2 inside(float m, int i, int D) {
+    if (VEC) return both(i < D ? m : 0.f);
+    return make_float2(i < D ? m : 0.f, i + 1 < D ? m : 0.f);
+}
+// The row less its mean.
+template <bool VEC, int G, int P>
+__device__ __forceinline__ void less_mean(Reduce<G>& red, float2 (&v)[P][4], int at, int threads, int D, float inv_d) {
+    float2 t = both(0.f);
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = (p * G + at) * 8 + j < D ? v[p][j] - m : 0.f;
-            q[0] += d * d;
-        }
-    red.template sum<1>(q);
-    *mean = m;
-    *rstd = 1.f / sqrtf(q[0] / (float)D + eps);
+        for (int j = 0; j < 4; ++j) t = add2(t, v[p][j]);   // (zeros outside the row)
+    float s[1] = {t.x + t.y};
+    red.template sum<1>(s);
+    const float m = -s[0] * inv_d;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[p][j] = add2(v[p][j], inside<VEC>(m, (p * threads + at) * 8 + 2 * j, D));
+}
+template <int P>
+__device__ __forceinline__ float square(const float2 (&v)[P][4]) {
+    float2 t = both(0.f);
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t = fma2(v[p][j], v[p][j], t);
+    return t.x + t.y;
 }
 
-// Threads of a unit, units of a block: G = 32 has eight warps to a block, each a unit.
-template <int G> constexpr int block_of() { return G == 32 ? 256 : G; }
+// What both passes begin with.  Units of up to a warp stay in step (their shuffles are the warp's): each goes through per_unit rows,
+// those behind its last one without a store.
+#define NORM_UNIT(A_, ...)                                                                                                              \
+    __shared__ __align__(16) float buf[Reduce<G>::kFloats];                                                                             \
+    __shared__ __align__(16) unsigned long long bars[kMaxStages + 4];                                                                   \
+    extern __shared__ __align__(128) unsigned char ring[];                                                                              \
+    const int threads = G <= 32 ? G : (int)blockDim.x, at = G <= 32 ? (int)threadIdx.x % G : (int)threadIdx.x;                          \
+    const int unit = G <= 32 ? (int)blockIdx.x * (256 / G) + (int)threadIdx.x / G : (int)blockIdx.x;                                    \
+    Reduce<G> red{buf, 0, (int)threadIdx.x >> 5, (int)threadIdx.x & 31};                                                                \
+    const int D = a.D, row0 = (int)min((long long)a.rows, (long long)unit * a.per_unit), row1 = min(a.rows - row0, a.per_unit) + row0;  \
+    const float inv_d = 1.f / (float)D;                                                                                                 \
+    RowFeed<T, VEC, G, P, A_> feed = {{__VA_ARGS__}};                                                                                   \
+    feed.at = at, feed.threads = threads, feed.D = D, feed.row0 = row0, feed.row1 = row1, feed.stages = a.stages, feed.limit = a.wait;  \
+    feed.ring = (unsigned)__cvta_generic_to_shared(ring), feed.zeros = (unsigned)__cvta_generic_to_shared(bars), feed.bars = feed.zeros + 32u; \
+    red.clear();                                                                                                                        \
+    feed.prepare();                                                                                                                     \
+    if (G > 32) __syncthreads();                                                                                                        \
+    rtoss_dev::pdl_enter()
 
 template <typename T, bool VEC, int G, int P>
-__global__ void __launch_bounds__(block_of<G>()) norm_forward_kernel(const NormArgs a) {
-    __shared__ float buf[4 * (G / 32)];
-    const int at = (int)threadIdx.x % G, unit = G == 32 ? (int)blockIdx.x * 8 + (int)threadIdx.x / 32 : (int)blockIdx.x;
-    Reduce<G> red{buf, 0, at / 32, (int)threadIdx.x & 31};
-    const int D = a.D;
-    rtoss_dev::pdl_enter();
-    const int row0 = unit * a.per_unit, row1 = min(a.rows, row0 + a.per_unit);
-    if (row0 >= row1) return;   // (a whole unit)
-    bool in[P];
-    float wpost[P][8], wpre[P][8], gate[P][8];
+__global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, false>()) norm_forward_kernel(const NormArgs a) {
+    NORM_UNIT(2, a.y, a.r);
+    feed.ld[0] = a.y_ld, feed.ld[1] = a.r_ld;
+    feed.start();
+    float2 wpost[P][4], wpre[P][4], gate[P][4];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int i = (p * G + at) * 8;
-        in[p] = i < D;
+        const int i = (p * threads + at) * 8;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            wpost[p][j] = a.wpost && i + j < D ? a.wpost[i + j] : 1.f;
-            wpre[p][j] = a.wpre && i + j < D ? a.wpre[i + j] : 1.f;
-            gate[p][j] = 1.f;
-        }
+        for (int j = 0; j < 4; ++j) wpost[p][j] = wpre[p][j] = gate[p][j] = both(1.f);
+        if (a.wpost && i < D) load8<float, VEC>(a.wpost, 0, 0, i, D, wpost[p]);
+        if (a.wpre && i < D) load8<float, VEC>(a.wpre, 0, 0, i, D, wpre[p]);
     }
-    int gate_row = -1;
-    float y[P][8], r[P][8];
-    Raw<T> yn[P], rn[P];   // of the next row
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        zero8(yn[p]);
-        zero8(rn[p]);
-    }
-    auto fetch = [&](int row) {
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (in[p]) {
-                fetch8<T, VEC>(a.y, a.y_ld, row, (p * G + at) * 8, D, yn[p]);
-                fetch8<T, VEC>(a.r, a.r_ld, row, (p * G + at) * 8, D, rn[p]);
-            }
-    };
-    fetch(row0);
-    for (int row = row0; row < row1; ++row) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            widen8<T>(yn[p], y[p]);
-            widen8<T>(rn[p], r[p]);
-        }
-        if (row + 1 < row1) fetch(row + 1);
-        if (a.gate && row / a.S != gate_row) {
-            gate_row = row / a.S;
+    int gate_row = row0 / a.S - 1, gate_at = row0;   // the gate at work, the row where the next one begins
+    const float2 scale = both(a.scale);
+    const int steps = G <= 32 ? a.per_unit : row1 - row0;
+    for (int k = 0; k < steps; ++k) {
+        const int row = row0 + k;
+        const bool live = G > 32 || row < row1;
+        float2 x[2][P][4];
+        feed.take(row, x);
+        float2(&y)[P][4] = x[0];
+        float2(&r)[P][4] = x[1];
+        if (a.gate && row == gate_at && live) {
+            ++gate_row;
+            gate_at = (gate_row + 1) * a.S;
 #pragma unroll
             for (int p = 0; p < P; ++p)
-                if (in[p]) load8<T, VEC>(a.gate, a.gate_ld, gate_row, (p * G + at) * 8, D, gate[p]);
+                if ((p * threads + at) * 8 < D) load8<T, VEC>(a.gate, a.gate_ld, gate_row, (p * threads + at) * 8, D, gate[p]);
         }
-        float mean = 0.f, rstd = 1.f;
-        if (a.post != RTOSS_NORM_NONE) stats<P, G>(red, y, in, at, D, a.post, a.eps, &mean, &rstd);
+        float2 rstd = both(1.f);
+        if (a.post != RTOSS_NORM_NONE) {
+            if (a.post == RTOSS_NORM_LAYER) less_mean<VEC, G, P>(red, y, at, threads, D, inv_d);
+            float s[1] = {square<P>(y)};
+            red.template sum<1>(s);
+            rstd = both(rsqrtf(s[0] * inv_d + a.eps));
+        }
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float v = (y[p][j] - mean) * rstd * wpost[p][j];
-                y[p][j] = (p * G + at) * 8 + j < D ? fmaf(gate[p][j], v, a.scale * r[p][j]) : 0.f;   // z
-            }
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (in[p]) store8<T, VEC>(a.z, a.z_ld, row, (p * G + at) * 8, D, y[p]);
+            for (int j = 0; j < 4; ++j) y[p][j] = fma2(gate[p][j], mul2(mul2(y[p][j], rstd), wpost[p][j]), mul2(scale, r[p][j]));   // z
+            if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.z, a.z_ld, row, (p * threads + at) * 8, D, y[p]);
+        }
         if (a.pre != RTOSS_NORM_NONE) {
-            stats<P, G>(red, y, in, at, D, a.pre, a.eps, &mean, &rstd);
+            if (a.pre == RTOSS_NORM_LAYER) less_mean<VEC, G, P>(red, y, at, threads, D, inv_d);
+            float s[1] = {square<P>(y)};
+            red.template sum<1>(s);
+            rstd = both(rsqrtf(s[0] * inv_d + a.eps));
 #pragma unroll
             for (int p = 0; p < P; ++p) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[p][j] = (y[p][j] - mean) * rstd * wpre[p][j];
-                if (in[p]) store8<T, VEC>(a.n, a.n_ld, row, (p * G + at) * 8, D, y[p]);
+                for (int j = 0; j < 4; ++j) y[p][j] = mul2(mul2(y[p][j], rstd), wpre[p][j]);
+                if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.n, a.n_ld, row, (p * threads + at) * 8, D, y[p]);
             }
+        } else if (feed.RING && a.post == RTOSS_NORM_NONE) {
+            __syncthreads();   // (the stage is free)
         }
     }
+    feed.finish(a.status);
 }
 
+// Four passes over the threads a row at most: mean of y; square of y; mean of z; square of z with the two sums that its norm's
+// gradient needs (they only lack the root, a factor); the two sums of the gradient of y's norm.
 template <typename T, bool VEC, int G, int P>
-__global__ void __launch_bounds__(block_of<G>()) norm_backward_kernel(const NormArgs a) {
-    __shared__ float buf[4 * (G / 32)];
-    const int at = (int)threadIdx.x % G, unit = G == 32 ? (int)blockIdx.x * 8 + (int)threadIdx.x / 32 : (int)blockIdx.x;
-    Reduce<G> red{buf, 0, at / 32, (int)threadIdx.x & 31};
-    const int D = a.D;
-    rtoss_dev::pdl_enter();
-    const int row0 = unit * a.per_unit, row1 = min(a.rows, row0 + a.per_unit);
-    if (row0 >= row1) return;
-    const float inv_d = 1.f / (float)D;
-    bool in[P];
-    float wpost[P][8], wpre[P][8], gate[P][8], s_post[P][8], s_pre[P][8], s_gate[P][8];
+__global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_backward_kernel(const NormArgs a) {
+    NORM_UNIT(4, a.y, a.r, a.dz, a.dn);
+    feed.ld[0] = a.y_ld, feed.ld[1] = a.r_ld, feed.ld[2] = a.dz_ld, feed.ld[3] = a.dn_ld;
+    feed.start();
+    constexpr bool kHold = P == 1;   // weights and gates stay in registers (else they are read again, from L1)
+    float2 wpost_[P][4], wpre_[P][4], gate_[P][4], s_post[P][4], s_pre[P][4], s_gate[P][4];
+    auto weights = [&](const float* w, int p, float2 (&v)[4]) {
+        const int i = (p * threads + at) * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = both(1.f);
+        if (w && i < D) load8<float, VEC>(w, 0, 0, i, D, v);
+    };
+    int gate_row = row0 / a.S - 1, gate_at = row0;
+    auto gates = [&](int p, float2 (&v)[4]) {
+        const int i = (p * threads + at) * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = both(1.f);
+        if (a.gate && i < D) load8<T, VEC>(a.gate, a.gate_ld, gate_row, i, D, v);
+    };
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int i = (p * G + at) * 8;
-        in[p] = i < D;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            wpost[p][j] = a.wpost && i + j < D ? a.wpost[i + j] : 1.f;
-            wpre[p][j] = a.wpre && i + j < D ? a.wpre[i + j] : 1.f;
-            gate[p][j] = 1.f;
-            s_post[p][j] = s_pre[p][j] = s_gate[p][j] = 0.f;
+        for (int j = 0; j < 4; ++j) {
+            s_post[p][j] = s_pre[p][j] = s_gate[p][j] = both(0.f);
+            gate_[p][j] = both(1.f);
+        }
+        if (kHold) {
+            weights(a.wpost, p, wpost_[p]);
+            weights(a.wpre, p, wpre_[p]);
         }
     }
-    int gate_row = -1;
-    float y[P][8], r[P][8], dz[P][8], dn[P][8];
-    Raw<T> yn[P], rn[P], dzn[P], dnn[P];   // of the next row
+    const float2 scale = both(a.scale);
+    const int steps = G <= 32 ? a.per_unit : row1 - row0;
+    for (int k = 0; k < steps; ++k) {
+        const int row = row0 + k;
+        const bool live = G > 32 || row < row1;
+        float2 x[4][P][4];
+        feed.take(row, x);
+        float2(&y)[P][4] = x[0];
+        float2(&z)[P][4] = x[1];
+        float2(&dz)[P][4] = x[2];
+        float2(&dn)[P][4] = x[3];
+        if (row == gate_at && live) {
+            ++gate_row;
+            gate_at = (gate_row + 1) * a.S;
+            if (kHold && a.gate) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        zero8(yn[p]);
-        zero8(rn[p]);
-        zero8(dzn[p]);
-        zero8(dnn[p]);
-    }
-    auto fetch = [&](int row) {
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (in[p]) {
-                const int i = (p * G + at) * 8;
-                fetch8<T, VEC>(a.y, a.y_ld, row, i, D, yn[p]);
-                fetch8<T, VEC>(a.r, a.r_ld, row, i, D, rn[p]);
-                if (a.dz) fetch8<T, VEC>(a.dz, a.dz_ld, row, i, D, dzn[p]);
-                if (a.dn) fetch8<T, VEC>(a.dn, a.dn_ld, row, i, D, dnn[p]);
+                for (int p = 0; p < P; ++p) gates(p, gate_[p]);
             }
-    };
-    fetch(row0);
-    for (int row = row0; row < row1; ++row) {
+        }
+        // y normalised and z again
+        float2 yrstd = both(1.f);
+        if (a.post != RTOSS_NORM_NONE) {
+            if (a.post == RTOSS_NORM_LAYER) less_mean<VEC, G, P>(red, y, at, threads, D, inv_d);
+            float s[1] = {square<P>(y)};
+            red.template sum<1>(s);
+            yrstd = both(rsqrtf(s[0] * inv_d + a.eps));
+        }
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            widen8<T>(yn[p], y[p]);
-            widen8<T>(rn[p], r[p]);
-            widen8<T>(dzn[p], dz[p]);
-            widen8<T>(dnn[p], dn[p]);
-        }
-        if (row + 1 < row1) fetch(row + 1);
-        if (a.gate && row / a.S != gate_row) {
-            gate_row = row / a.S;
+            float2 w_[4], g_[4];
+            if (!kHold) weights(a.wpost, p, w_), gates(p, g_);
+            float2(&w)[4] = kHold ? wpost_[p] : w_;
+            float2(&g)[4] = kHold ? gate_[p] : g_;
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-                if (in[p]) load8<T, VEC>(a.gate, a.gate_ld, gate_row, (p * G + at) * 8, D, gate[p]);
-        }
-        // v and z again
-        float ymean = 0.f, yrstd = 1.f, zmean = 0.f, zrstd = 1.f;
-        if (a.post != RTOSS_NORM_NONE) stats<P, G>(red, y, in, at, D, a.post, a.eps, &ymean, &yrstd);
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool here = (p * G + at) * 8 + j < D;
-                y[p][j] = here ? (y[p][j] - ymean) * yrstd : 0.f;   // y normalised
-                r[p][j] = here ? fmaf(gate[p][j], y[p][j] * wpost[p][j], a.scale * r[p][j]) : 0.f;   // z
+            for (int j = 0; j < 4; ++j) {
+                y[p][j] = mul2(y[p][j], yrstd);
+                z[p][j] = fma2(g[j], mul2(y[p][j], w[j]), mul2(scale, z[p][j]));
             }
+        }
         if (a.pre != RTOSS_NORM_NONE) {
-            stats<P, G>(red, r, in, at, D, a.pre, a.eps, &zmean, &zrstd);
-            float m[2] = {0.f, 0.f};
+            if (a.pre == RTOSS_NORM_LAYER) less_mean<VEC, G, P>(red, z, at, threads, D, inv_d);
+            float2 q = both(0.f), b = both(0.f), c = both(0.f);
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+            for (int p = 0; p < P; ++p) {
+                float2 w_[4];
+                if (!kHold) weights(a.wpre, p, w_);
+                float2(&w)[4] = kHold ? wpre_[p] : w_;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float hat = (p * G + at) * 8 + j < D ? (r[p][j] - zmean) * zrstd : 0.f, gn = dn[p][j] * wpre[p][j];
-                    s_pre[p][j] += dn[p][j] * hat;
-                    r[p][j] = hat;
-                    m[0] += gn * hat;
-                    m[1] += gn;
+                for (int j = 0; j < 4; ++j) {
+                    const float2 g = mul2(dn[p][j], w[j]);
+                    q = fma2(z[p][j], z[p][j], q);
+                    b = fma2(g, z[p][j], b);
+                    c = add2(c, g);
                 }
-            red.template sum<2>(m);
-            const float m0 = m[0] * inv_d, m1 = a.pre == RTOSS_NORM_LAYER ? m[1] * inv_d : 0.f;
+            }
+            float s[3] = {q.x + q.y, b.x + b.y, c.x + c.y};
+            red.template sum<3>(s);
+            const float rstd = rsqrtf(s[0] * inv_d + a.eps);
+            const float2 zrstd = both(rstd), m0 = both(-(s[1] * rstd) * inv_d);
+            const float m1 = a.pre == RTOSS_NORM_LAYER ? -s[2] * inv_d : 0.f;
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+            for (int p = 0; p < P; ++p) {
+                float2 w_[4];
+                if (!kHold) weights(a.wpre, p, w_);
+                float2(&w)[4] = kHold ? wpre_[p] : w_;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dz[p][j] += zrstd * (dn[p][j] * wpre[p][j] - r[p][j] * m0 - m1);
+                for (int j = 0; j < 4; ++j) {
+                    const float2 hat = mul2(z[p][j], zrstd);
+                    if (live) s_pre[p][j] = fma2(dn[p][j], hat, s_pre[p][j]);
+                    const float2 g = fma2(hat, m0, fma2(dn[p][j], w[j], inside<VEC>(m1, (p * threads + at) * 8 + 2 * j, D)));
+                    dz[p][j] = fma2(zrstd, g, dz[p][j]);
+                }
+            }
         }
         // dz holds the whole gradient of z
-        float m[2] = {0.f, 0.f};
+        float2 b = both(0.f), c = both(0.f);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            float out[8];
+            float2 out[4], w_[4], g_[4];
+            if (!kHold) weights(a.wpost, p, w_), gates(p, g_);
+            float2(&w)[4] = kHold ? wpost_[p] : w_;
+            float2(&g)[4] = kHold ? gate_[p] : g_;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                out[j] = a.scale * dz[p][j];
-                s_gate[p][j] += dz[p][j] * (y[p][j] * wpost[p][j]);
-                const float dv = dz[p][j] * gate[p][j];
-                s_post[p][j] += dv * y[p][j];
-                dz[p][j] = dv * wpost[p][j];
-                m[0] += dz[p][j] * y[p][j];
-                m[1] += (p * G + at) * 8 + j < D ? dz[p][j] : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                out[j] = mul2(scale, dz[p][j]);
+                const float2 v = mul2(y[p][j], w[j]), dv = mul2(dz[p][j], g[j]);
+                if (live) {
+                    s_gate[p][j] = fma2(dz[p][j], v, s_gate[p][j]);
+                    s_post[p][j] = fma2(dv, y[p][j], s_post[p][j]);
+                }
+                b = fma2(dv, v, b);
+                dz[p][j] = mul2(dv, w[j]);
+                c = add2(c, dz[p][j]);
             }
-            if (in[p]) store8<T, VEC>(a.dr, a.dr_ld, row, (p * G + at) * 8, D, out);
+            if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.dr, a.dr_ld, row, (p * threads + at) * 8, D, out);
         }
         if (a.post != RTOSS_NORM_NONE) {
-            red.template sum<2>(m);
-            const float m0 = m[0] * inv_d, m1 = a.post == RTOSS_NORM_LAYER ? m[1] * inv_d : 0.f;
+            float s[2] = {b.x + b.y, c.x + c.y};
+            red.template sum<2>(s);
+            const float2 m0 = both(-s[0] * inv_d), m1 = both(a.post == RTOSS_NORM_LAYER ? -s[1] * inv_d : 0.f);
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dz[p][j] = yrstd * (dz[p][j] - y[p][j] * m0 - m1);
+                for (int j = 0; j < 4; ++j) dz[p][j] = mul2(yrstd, add2(fma2(y[p][j], m0, dz[p][j]), m1));
+        } else if (feed.RING && a.pre == RTOSS_NORM_NONE) {
+            __syncthreads();   // (the stage is free)
         }
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (in[p]) store8<T, VEC>(a.dy, a.dy_ld, row, (p * G + at) * 8, D, dz[p]);
+            if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.dy, a.dy_ld, row, (p * threads + at) * 8, D, dz[p]);
         // a gate's last row here: its sum is final when all its rows were this unit's, else one of the unit's two shares
-        if (a.dgate && (row + 1 == row1 || (row + 1) / a.S != row / a.S)) {
-            const int first = row / a.S * a.S, last = first + a.S;   // (S divides the tokens)
-            const bool whole = first >= row0 && last <= row1;
+        if (a.dgate && live && (row + 1 == row1 || row + 1 == gate_at)) {
+            const int first = gate_at - a.S;   // (S divides the tokens)
+            const bool whole = first >= row0 && gate_at <= row1;
             float* part = a.p_gate + ((long long)unit * 2 + (first > row0 ? 1 : 0)) * D;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int i = (p * G + at) * 8;
-                if (in[p]) {
-                    if (whole) store8<T, VEC>(a.dgate, a.dgate_ld, row / a.S, i, D, s_gate[p]);
+                const int i = (p * threads + at) * 8;
+                if (i < D) {
+                    if (whole) store8<T, VEC>(a.dgate, a.dgate_ld, gate_row, i, D, s_gate[p]);
                     else store8<float, VEC>(part, 0, 0, i, D, s_gate[p]);
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s_gate[p][j] = 0.f;
+                for (int j = 0; j < 4; ++j) s_gate[p][j] = both(0.f);
             }
         }
     }
+    if constexpr (G <= 32) {
+        // the block's units, added in their order
+        __shared__ float2 part[256][4];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const int i = (p * G + at) * 8;
-        if (!in[p]) continue;
-        if (a.p_post) store8<float, VEC>(a.p_post, D, unit, i, D, s_post[p]);
-        if (a.p_pre) store8<float, VEC>(a.p_pre, D, unit, i, D, s_pre[p]);
+        for (int what = 0; what < 2; ++what) {
+            float* to = what ? a.p_pre : a.p_post;
+            if (!to) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[threadIdx.x][j] = what ? s_pre[0][j] : s_post[0][j];
+            __syncthreads();
+            for (int i = (int)threadIdx.x; i < D; i += 256) {
+                float t = 0.f;
+#pragma unroll 8
+                for (int u = 0; u < 256 / G; ++u) t += reinterpret_cast<const float*>(part[u * G])[i];
+                to[(long long)blockIdx.x * D + i] = t;
+            }
+            __syncthreads();
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int i = (p * threads + at) * 8;
+            if (i >= D) continue;
+            if (a.p_post) store8<float, VEC>(a.p_post, D, unit, i, D, s_post[p]);
+            if (a.p_pre) store8<float, VEC>(a.p_pre, D, unit, i, D, s_pre[p]);
+        }
     }
+    feed.finish(a.status);
 }
 
 // ---- rows of more than 8192 values: a block a run of rows, every pass reads them again (from the caches) -----------------
@@ -379,7 +619,7 @@ __device__ __forceinline__ float at_of(const void* base, long long ld, int row, 
 
 template <typename T, bool BACKWARD>
 __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormArgs a) {
-    __shared__ float buf[4 * (kLongThreads / 32)];
+    __shared__ __align__(16) float buf[Reduce<kLongThreads>::kFloats];
     Reduce<kLongThreads> red{buf, 0, (int)threadIdx.x / 32, (int)threadIdx.x & 31};
     rtoss_dev::pdl_enter();
     const int unit = (int)blockIdx.x, row0 = unit * a.per_unit, row1 = min(a.rows, row0 + a.per_unit), D = a.D, tid = (int)threadIdx.x;
@@ -482,19 +722,18 @@ struct JoinArgs {
     float *dpost, *dpre;
     void* dgate;
     long long dgate_ld;
-    int D, units, per_unit, S, by_gate;
+    int D, parts, per_unit, S, by_gate;   // parts: rows of p_post and p_pre
 };
 
-// 32 columns a block, 32 runs of units side by side, joined in their order.
+// 32 threads with four columns each a block, 32 runs of units side by side, joined in their order.
 constexpr int kJoinRuns = 32;
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArgs a) {
-    __shared__ float s[kJoinRuns][32];
+    __shared__ float4 s[kJoinRuns][32];
     rtoss_dev::pdl_enter();
-    const int col = (int)blockIdx.x * 32 + ((int)threadIdx.x & 31), run = (int)threadIdx.x >> 5, what = (int)blockIdx.y;
-    const bool in = col < a.D;
+    const int col = (int)blockIdx.x * 128 + ((int)threadIdx.x & 31) * 4, run = (int)threadIdx.x >> 5, what = (int)blockIdx.y;
     const float* p = what == 0 ? a.p_post : a.p_pre;
-    int first = 0, last = a.units;   // units that hold a share
+    int first = 0, last = a.parts;   // rows that hold a share
     long long pitch = a.D;
     long long row0 = 0;   // first row of the gate
     if (what >= 2) {
@@ -511,72 +750,98 @@ __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArg
         return;
     }
     const int each = (last - first + kJoinRuns - 1) / kJoinRuns, lo = first + run * each, hi = min(last, lo + each);
-    float sum = 0.f;
-    if (in)
-#pragma unroll 4
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4& w) { sum.x += w.x, sum.y += w.y, sum.z += w.z, sum.w += w.w; };
+    if (col < a.D) {
+#pragma unroll 5
         for (int u = lo; u < hi; ++u) {
             // (a gate that begins inside a unit is that unit's second share)
             const long long second = what >= 2 && row0 > (long long)u * a.per_unit ? a.D : 0;
-            sum += p[u * pitch + second + col];
+            const float* at = p + u * pitch + second + col;
+            if (VEC) add(*reinterpret_cast<const float4*>(at));
+            else add(make_float4(at[0], col + 1 < a.D ? at[1] : 0.f, col + 2 < a.D ? at[2] : 0.f, col + 3 < a.D ? at[3] : 0.f));
         }
+    }
     s[run][threadIdx.x & 31] = sum;
     __syncthreads();
-    if (run == 0 && in) {
-        sum = 0.f;
+    if (run < 4) {   // a column a thread
+        const int c = (int)threadIdx.x, at = (int)blockIdx.x * 128 + c;
+        float t = 0.f;
 #pragma unroll
-        for (int k = 0; k < kJoinRuns; ++k) sum += s[k][threadIdx.x & 31];
-        if (what == 0) a.dpost[col] = sum;
-        else if (what == 1) a.dpre[col] = sum;
-        else reinterpret_cast<T*>(a.dgate)[row0 / a.S * a.dgate_ld + col] = from_f32<T>(sum);
+        for (int k = 0; k < kJoinRuns; ++k) t += reinterpret_cast<const float*>(s[k])[c];
+        if (at >= a.D) return;
+        if (what == 0) a.dpost[at] = t;
+        else if (what == 1) a.dpre[at] = t;
+        else reinterpret_cast<T*>(a.dgate)[row0 / a.S * a.dgate_ld + at] = from_f32<T>(t);
     }
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
 // How rows are dealt out: threads of a unit by the row's length, units by what the device holds at once.
 struct Plan {
-    int G, P, units, per_unit;
+    int G, P, threads, blocks, units, per_unit;   // threads: of a block; blocks: of an SM
+    int parts;                                    // rows of partial sums: one a block
 };
 Plan plan_of(int64_t rows, int D, int sms, bool backward) {
     Plan p;
-    if (D <= 256) p.G = 32, p.P = 1;
-    else if (D <= 1024) p.G = 128, p.P = 1;
-    else if (D <= 2048) p.G = 256, p.P = 1;
-    else if (D <= 4096) p.G = 512, p.P = 1;
-    else if (D <= 8192) p.G = 512, p.P = 2;
-    else p.G = kLongThreads, p.P = 0;
-    const int64_t most = (int64_t)sms * (backward ? (p.G == 32 ? 16 : p.G == 128 ? 4 : p.G == 256 ? 2 : 1) : p.G == 32 ? 32 : 1024 / p.G);
+    const int pieces = (D + 7) / 8, room = backward ? 512 : 1024;
+    p.P = D <= 4096 ? 1 : D <= 8192 ? 2 : 0;
+    p.G = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : pieces <= 128 ? 128 : pieces <= 256 ? 256 : 512;
+    if (p.P == 0) p.G = p.threads = kLongThreads, p.blocks = backward ? 1 : 2;
+    else if (p.G <= 32) p.threads = 256, p.blocks = room / 256;
+    else p.threads = ((pieces + p.P - 1) / p.P + 31) / 32 * 32, p.blocks = (p.P == 2 ? 512 : room) / p.threads;
+    const int per_block = p.P && p.G <= 32 ? 256 / p.G : 1;
+    const int64_t most = (int64_t)sms * p.blocks * per_block;
     const int64_t units = rows < most ? rows : most;
     p.per_unit = (int)((rows + units - 1) / units);
     p.units = (int)((rows + p.per_unit - 1) / p.per_unit);
+    p.parts = (p.units + per_block - 1) / per_block;
     return p;
 }
 
-template <typename T, bool VEC, bool BACKWARD>
-int launch_as(const Plan& p, const NormArgs& a, cudaStream_t s) {
-    const unsigned grid = (unsigned)(p.G == 32 ? (p.units + 7) / 8 : p.units);
-    auto go = [&](auto kernel, int threads) { return (int)rtoss_dev::launch_pdl(kernel, grid, (unsigned)threads, 0, s, a); };
-    if (p.P == 0) return go(norm_long_kernel<T, BACKWARD>, kLongThreads);
-    if (BACKWARD) {
-        if (p.G == 32) return go(norm_backward_kernel<T, VEC, 32, 1>, 256);
-        if (p.G == 128) return go(norm_backward_kernel<T, VEC, 128, 1>, 128);
-        if (p.G == 256) return go(norm_backward_kernel<T, VEC, 256, 1>, 256);
-        if (p.P == 1) return go(norm_backward_kernel<T, VEC, 512, 1>, 512);
-        return go(norm_backward_kernel<T, VEC, 512, 2>, 512);
+template <typename T, bool VEC, int G, int P, bool BACKWARD>
+int launch_one(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s) {
+    auto kernel = [] {
+        if constexpr (BACKWARD) return norm_backward_kernel<T, VEC, G, P>;
+        else return norm_forward_kernel<T, VEC, G, P>;
+    }();
+    int smem = 0;
+    if constexpr (VEC && G > 32) {
+        // an SM's 227 KB, less a kilobyte of the system's and one of a block's own
+        const int stage = a.D * (int)sizeof(T) * (BACKWARD ? 4 : 2), room = 227 * 1024 / p.blocks - 2 * 1024;
+        int n = room / stage;
+        n = n < kMaxStages ? n : kMaxStages;
+        a.stages = n < p.per_unit ? n : p.per_unit;
+        smem = a.stages * stage;
+        static std::atomic<bool> allowed[64];
+        const int dev = ctx->device;
+        if (smem > 40 * 1024 && (dev >= 64 || !allowed[dev].load(std::memory_order_acquire))) {
+            if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024)) return (int)e;
+            if (dev < 64) allowed[dev].store(true, std::memory_order_release);
+        }
     }
-    if (p.G == 32) return go(norm_forward_kernel<T, VEC, 32, 1>, 256);
-    if (p.G == 128) return go(norm_forward_kernel<T, VEC, 128, 1>, 128);
-    if (p.G == 256) return go(norm_forward_kernel<T, VEC, 256, 1>, 256);
-    if (p.P == 1) return go(norm_forward_kernel<T, VEC, 512, 1>, 512);
-    return go(norm_forward_kernel<T, VEC, 512, 2>, 512);
+    return (int)rtoss_dev::launch_pdl(kernel, (unsigned)p.parts, (unsigned)p.threads, (size_t)smem, s, a);
+}
+
+template <typename T, bool VEC, bool BACKWARD>
+int launch_as(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s) {
+    if (p.G == 8) return launch_one<T, VEC, 8, 1, BACKWARD>(ctx, p, a, s);
+    if (p.G == 16) return launch_one<T, VEC, 16, 1, BACKWARD>(ctx, p, a, s);
+    if (p.G == 32) return launch_one<T, VEC, 32, 1, BACKWARD>(ctx, p, a, s);
+    if (p.G == 128) return launch_one<T, VEC, 128, 1, BACKWARD>(ctx, p, a, s);
+    if (p.G == 256) return launch_one<T, VEC, 256, 1, BACKWARD>(ctx, p, a, s);
+    if (p.P == 1) return launch_one<T, VEC, 512, 1, BACKWARD>(ctx, p, a, s);
+    return launch_one<T, VEC, 512, 2, BACKWARD>(ctx, p, a, s);
 }
 
 template <typename T, bool BACKWARD>
-int launch(const Plan& p, const NormArgs& a, cudaStream_t s) {
-    return a.vec ? launch_as<T, true, BACKWARD>(p, a, s) : launch_as<T, false, BACKWARD>(p, a, s);
+int launch(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s) {
+    if (p.P == 0) return (int)rtoss_dev::launch_pdl(norm_long_kernel<T, BACKWARD>, (unsigned)p.parts, (unsigned)kLongThreads, 0, s, a);
+    return a.vec ? launch_as<T, true, BACKWARD>(ctx, p, a, s) : launch_as<T, false, BACKWARD>(ctx, p, a, s);
 }
 
 bool norm_ok(int k) { return k == RTOSS_NORM_NONE || k == RTOSS_NORM_RMS || k == RTOSS_NORM_LAYER; }
-int64_t ws_floats(const Plan& p, int D, bool gated) { return (int64_t)p.units * D * (gated ? 4 : 2); }
+int64_t ws_floats(const Plan& p, int D, bool gated) { return 2ll * p.parts * D + (gated ? 2ll * p.units * D : 0); }
 
 rtoss_status check(rtoss_ctx* ctx, const rtoss_block_norm* b, bool backward, const char* where) {
     if (!ctx) return RTOSS_ERR_INVALID_ARG;
@@ -602,7 +867,7 @@ rtoss_status check(rtoss_ctx* ctx, const rtoss_block_norm* b, bool backward, con
 }
 
 // Rows that can be moved 16 bytes at a time: D, strides and bases are multiples of what eight values (four fp32 ones) take.
-NormArgs args_of(const rtoss_block_norm* b, const Plan& p, bool backward) {
+NormArgs args_of(const rtoss_ctx* ctx, const rtoss_block_norm* b, const Plan& p, bool backward) {
     NormArgs a = {};
     const int es = (int)rtoss_dtype_size(b->dtype);
     bool vec = b->D % 8 == 0;
@@ -618,27 +883,31 @@ NormArgs args_of(const rtoss_block_norm* b, const Plan& p, bool backward) {
         a.z = take(b->z, &a.z_ld), a.n = take(b->n, &a.n_ld);
     }
     a.wpost = b->post_weight_dev, a.wpre = b->pre_weight_dev;
+    if (!aligned16(a.wpost) || !aligned16(a.wpre)) vec = false;
     a.rows = (int)b->tokens, a.D = b->D, a.post = b->post, a.pre = b->pre, a.vec = vec;
-    a.S = b->gate.dev ? (int)b->tokens_per_gate : 1;
+    a.S = b->gate.dev ? (int)b->tokens_per_gate : (int)b->tokens;
     a.per_unit = p.per_unit;
     a.scale = b->residual_scale, a.eps = b->eps;
+    a.status = ctx->dev_status, a.wait = ctx->wait_cycles > 0 ? ctx->wait_cycles : 2000000000ll;
     return a;
 }
 
 template <typename T>
-int backward(const rtoss_block_norm* b, const Plan& p, cudaStream_t s) {
-    NormArgs a = args_of(b, p, true);
+int backward(const rtoss_ctx* ctx, const rtoss_block_norm* b, const Plan& p, cudaStream_t s) {
+    NormArgs a = args_of(ctx, b, p, true);
     float* ws = b->workspace_dev;
-    const int64_t part = (int64_t)p.units * b->D;
+    const int64_t part = (int64_t)p.parts * b->D;
     a.p_post = b->dpost_weight_dev ? ws : nullptr;
     a.p_pre = b->dpre_weight_dev ? ws + part : nullptr;
     a.p_gate = b->dgate.dev ? ws + 2 * part : nullptr;
-    if (const int e = launch<T, true>(p, a, s)) return e;
+    if (const int e = launch<T, true>(ctx, p, a, s)) return e;
     const bool join_gates = a.dgate && p.units > 1 && p.per_unit % a.S != 0;   // (else every gate's rows were one unit's)
     if (!a.p_post && !a.p_pre && !join_gates) return 0;
     const int gates = (int)(b->tokens / a.S), by_gate = gates < p.units;
-    JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.units, p.per_unit, a.S, by_gate};
-    return (int)rtoss_dev::launch_pdl(norm_join_kernel<T>, dim3((unsigned)((b->D + 31) / 32), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.units - 1))), dim3(kJoinRuns * 32), 0, s, j);
+    JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.parts, p.per_unit, a.S, by_gate};
+    const dim3 grid((unsigned)((b->D + 127) / 128), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.units - 1)));
+    return b->D % 4 == 0 ? (int)rtoss_dev::launch_pdl(norm_join_kernel<T, true>, grid, dim3(kJoinRuns * 32), 0, s, j)
+                         : (int)rtoss_dev::launch_pdl(norm_join_kernel<T, false>, grid, dim3(kJoinRuns * 32), 0, s, j);
 }
 
 }  // namespace
@@ -651,8 +920,8 @@ rtoss_status rtoss_block_norm_forward(rtoss_ctx* ctx, const rtoss_block_norm* b,
     rtoss_device_guard on_device(ctx->device);
     cudaStream_t s = (cudaStream_t)cuda_stream;
     const Plan p = plan_of(b->tokens, b->D, ctx->sm_count > 0 ? ctx->sm_count : 148, false);
-    const NormArgs a = args_of(b, p, false);
-    return launched(ctx, kFwd, b->dtype == RTOSS_F32 ? launch<float, false>(p, a, s) : b->dtype == RTOSS_BF16 ? launch<__nv_bfloat16, false>(p, a, s) : launch<__half, false>(p, a, s));
+    NormArgs a = args_of(ctx, b, p, false);
+    return launched(ctx, kFwd, b->dtype == RTOSS_F32 ? launch<float, false>(ctx, p, a, s) : b->dtype == RTOSS_BF16 ? launch<__nv_bfloat16, false>(ctx, p, a, s) : launch<__half, false>(ctx, p, a, s));
 }
 
 rtoss_status rtoss_block_norm_workspace(const rtoss_ctx* ctx, int64_t tokens, int D, int gated, int64_t* floats) {
@@ -677,7 +946,7 @@ rtoss_status rtoss_block_norm_backward(rtoss_ctx* ctx, const rtoss_block_norm* b
         if (!aligned16(b->workspace_dev)) return fail(ctx, RTOSS_ERR_ALIGNMENT, kBwd, "the workspace must be 16-byte aligned");
         if (b->workspace_floats < ws_floats(p, b->D, b->dgate.dev != nullptr)) return fail(ctx, RTOSS_ERR_INVALID_ARG, kBwd, "workspace too small");
     }
-    return launched(ctx, kBwd, b->dtype == RTOSS_F32 ? backward<float>(b, p, s) : b->dtype == RTOSS_BF16 ? backward<__nv_bfloat16>(b, p, s) : backward<__half>(b, p, s));
+    return launched(ctx, kBwd, b->dtype == RTOSS_F32 ? backward<float>(ctx, b, p, s) : b->dtype == RTOSS_BF16 ? backward<__nv_bfloat16>(ctx, b, p, s) : backward<__half>(ctx, b, p, s));
 }
 
 }  // extern "C"
