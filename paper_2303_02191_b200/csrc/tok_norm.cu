@@ -176,10 +176,12 @@ struct Reduce {
 // Units of a block: those of up to a warp share a block of 256 threads, larger ones are blocks of up to G threads (as many warps
 // as the row has pieces for).
 template <int G> constexpr int block_of() { return G <= 32 ? 256 : G; }
-// Blocks of G threads that an SM holds: the forward pass has 64 registers a thread, the backward pass, whose sums over tokens
-// stay in them, 128.
+// Threads that an SM holds, by the registers of one (64, 80 or 128): the backward pass keeps its sums over tokens in them, units of
+// up to a warp the next row, and P = 2 has twice the columns.
 template <int G, int P, bool BACKWARD>
-constexpr int blocks_of() { return (BACKWARD || P == 2 ? 512 : 1024) / block_of<G>(); }
+constexpr int threads_of() { return P == 2 || (BACKWARD && G <= 32) ? 512 : BACKWARD ? 768 : 1024; }
+template <int G, int P, bool BACKWARD>
+constexpr int blocks_of() { return threads_of<G, P, BACKWARD>() / block_of<G>(); }
 
 // Rows on their way to a unit, A operands of each.  RING: a block's rows come by bulk copies through a ring of stages in shared
 // memory, up to `stages` rows ahead of the one at work (with one row ahead in registers an SM had 32 KB in flight, too little
@@ -192,12 +194,12 @@ struct RowFeed {
     long long ld[A];
     int at, threads, D, row0, row1, stages;
     // ring
-    unsigned ring, bars, zeros, row_bytes, stage_bytes, tx;
+    unsigned ring, bars, zeros, row_bytes, stage_bytes, tx, from;
     int s, s_fill, fill;   // stage of the row at work; stage and row to ask for next
     unsigned phase;
     bool dead;
     long long limit;
-    Raw<T> next[RING ? 1 : A][RING ? 1 : P];
+    Raw<T> now[RING ? 1 : A][RING ? 1 : P], next[RING ? 1 : A][RING ? 1 : P];
 
     __device__ __forceinline__ void ask() {   // (thread 0)
         const unsigned bar = bars + 8u * (unsigned)s_fill, to = ring + (unsigned)s_fill * stage_bytes;
@@ -257,8 +259,8 @@ struct RowFeed {
             : "memory");
         return done;
     }
-    // The row's values.  RING: between two calls the block has met at a barrier, so the stage of the row before is free.
-    __device__ __forceinline__ void take(int row, float2 (&v)[A][P][4]) {
+    // The row is here.  RING: the block has met at a barrier since the row before was last read, so that one's stage is free.
+    __device__ __forceinline__ void begin(int row) {
         if constexpr (RING) {
             if (threadIdx.x == 0 && row > row0 && fill < row1 && !dead) ask();
             const unsigned bar = bars + 8u * (unsigned)s;
@@ -270,28 +272,33 @@ struct RowFeed {
                         break;
                     }
             }
-            const unsigned from = ring + (unsigned)s * stage_bytes;
-#pragma unroll
-            for (int k = 0; k < A; ++k)
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    Raw<T> r;
-                    const unsigned i = (unsigned)(p * threads + at) * 8u;
-                    const unsigned a = base[k] && i < (unsigned)D ? from + (unsigned)k * row_bytes + i * (unsigned)sizeof(T) : zeros;
-#pragma unroll
-                    for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
-                        uint4& w = reinterpret_cast<uint4*>(&r)[j];
-                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a + 16u * j) : "memory");
-                    }
-                    widen8<T>(r, v[k][p]);
-                }
+            from = ring + (unsigned)s * stage_bytes;
             if (++s == stages) s = 0, phase ^= 1u;
         } else {
 #pragma unroll
             for (int k = 0; k < A; ++k)
 #pragma unroll
-                for (int p = 0; p < P; ++p) widen8<T>(next[k][p], v[k][p]);
+                for (int p = 0; p < P; ++p) now[k][p] = next[k][p];
             if (row + 1 < row1) prefetch(row + 1);
+        }
+    }
+    // Operand k of it.  (RING: read where it is needed, which keeps the registers free until then)
+    __device__ __forceinline__ void get(int k, float2 (&v)[P][4]) const {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if constexpr (RING) {
+                Raw<T> r;
+                const unsigned i = (unsigned)(p * threads + at) * 8u;
+                const unsigned a = base[k] && i < (unsigned)D ? from + (unsigned)k * row_bytes + i * (unsigned)sizeof(T) : zeros;
+#pragma unroll
+                for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+                    uint4& w = reinterpret_cast<uint4*>(&r)[j];
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(a + 16u * j) : "memory");
+                }
+                widen8<T>(r, v[p]);
+            } else {
+                widen8<T>(now[k][p], v[p]);
+            }
         }
     }
     // A wait that ran out is told to the host; the copies on their way land before the block ends.
@@ -307,9 +314,9 @@ struct RowFeed {
 
 // A number, in the places of the thread's piece that lie inside the row (else 0).
 template <bool VEC>
-__device__ __forceinline__ float2 inside(float m, int i, int D) {
+__device__ __forceinline__ float2 inside(float m, int i, int j, int D) {   // values 2j and 2j + 1 of the piece from column i on
     if (VEC) return both(i < D ? m : 0.f);
-    return make_float2(i < D ? m : 0.f, i + 1 < D ? m : 0.f);
+    return make_float2(i + 2 * j < D ? m : 0.f, i + 2 * j + 1 < D ? m : 0.f);
 }
 // The row less its mean.
 template <bool VEC, int G, int P>
@@ -325,7 +332,7 @@ __device__ __forceinline__ void less_mean(Reduce<G>& red, float2 (&v)[P][4], int
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[p][j] = add2(v[p][j], inside<VEC>(m, (p * threads + at) * 8 + 2 * j, D));
+        for (int j = 0; j < 4; ++j) v[p][j] = add2(v[p][j], inside<VEC>(m, (p * threads + at) * 8, j, D));
 }
 template <int P>
 __device__ __forceinline__ float square(const float2 (&v)[P][4]) {
@@ -376,10 +383,10 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, false>()) norm_
     for (int k = 0; k < steps; ++k) {
         const int row = row0 + k;
         const bool live = G > 32 || row < row1;
-        float2 x[2][P][4];
-        feed.take(row, x);
-        float2(&y)[P][4] = x[0];
-        float2(&r)[P][4] = x[1];
+        float2 y[P][4], r[P][4];
+        feed.begin(row);
+        feed.get(0, y);
+        feed.get(1, r);
         if (a.gate && row == gate_at && live) {
             ++gate_row;
             gate_at = (gate_row + 1) * a.S;
@@ -420,20 +427,24 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, false>()) norm_
 
 // Four passes over the threads a row at most: mean of y; square of y; mean of z; square of z with the two sums that its norm's
 // gradient needs (they only lack the root, a factor); the two sums of the gradient of y's norm.
+// The gate and the weight of y's norm only ever come as their product, and the sums for both are one, A = sum of dz * yhat over
+// the rows that share a gate: dgate = weight * A, and dpost_weight gets gate * A.  So a thread holds four values for each of
+// its columns instead of six, and three blocks of 256 threads fit an SM.
 template <typename T, bool VEC, int G, int P>
 __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_backward_kernel(const NormArgs a) {
     NORM_UNIT(4, a.y, a.r, a.dz, a.dn);
     feed.ld[0] = a.y_ld, feed.ld[1] = a.r_ld, feed.ld[2] = a.dz_ld, feed.ld[3] = a.dn_ld;
     feed.start();
-    constexpr bool kHold = P == 1;   // weights and gates stay in registers (else they are read again, from L1)
-    float2 wpost_[P][4], wpre_[P][4], gate_[P][4], s_post[P][4], s_pre[P][4], s_gate[P][4];
+    float2 gw[P][4], wpre[P][4], s_all[P][4], s_pre[P][4], s_post[G <= 32 ? P : 1][4];
+    // (G > 32: the sums for post_weight lie behind the ring, a thread's own columns)
+    float2* const post_sum = reinterpret_cast<float2*>(ring + (feed.RING ? a.stages * 4 * D * (int)sizeof(T) : 0)) + at * 4;
     auto weights = [&](const float* w, int p, float2 (&v)[4]) {
         const int i = (p * threads + at) * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = both(1.f);
         if (w && i < D) load8<float, VEC>(w, 0, 0, i, D, v);
     };
-    int gate_row = row0 / a.S - 1, gate_at = row0;
+    int gate_row = row0 / a.S - 1, gate_at = row0;   // the gate at work, the row where the next one begins
     auto gates = [&](int p, float2 (&v)[4]) {
         const int i = (p * threads + at) * 8;
 #pragma unroll
@@ -442,14 +453,12 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
     };
 #pragma unroll
     for (int p = 0; p < P; ++p) {
+        weights(a.wpre, p, wpre[p]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            s_post[p][j] = s_pre[p][j] = s_gate[p][j] = both(0.f);
-            gate_[p][j] = both(1.f);
-        }
-        if (kHold) {
-            weights(a.wpost, p, wpost_[p]);
-            weights(a.wpre, p, wpre_[p]);
+            s_all[p][j] = s_pre[p][j] = gw[p][j] = both(0.f);
+            if constexpr (G <= 32) s_post[p][j] = both(0.f);
+            else post_sum[p * threads * 4 + j] = both(0.f);
         }
     }
     const float2 scale = both(a.scale);
@@ -457,21 +466,22 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
     for (int k = 0; k < steps; ++k) {
         const int row = row0 + k;
         const bool live = G > 32 || row < row1;
-        float2 x[4][P][4];
-        feed.take(row, x);
-        float2(&y)[P][4] = x[0];
-        float2(&z)[P][4] = x[1];
-        float2(&dz)[P][4] = x[2];
-        float2(&dn)[P][4] = x[3];
+        float2 y[P][4], z[P][4], dn[P][4], dz[P][4];
+        feed.begin(row);
         if (row == gate_at && live) {
             ++gate_row;
             gate_at = (gate_row + 1) * a.S;
-            if (kHold && a.gate) {
 #pragma unroll
-                for (int p = 0; p < P; ++p) gates(p, gate_[p]);
+            for (int p = 0; p < P; ++p) {
+                float2 w[4], g[4];
+                weights(a.wpost, p, w);
+                gates(p, g);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) gw[p][j] = mul2(g[j], w[j]);
             }
         }
         // y normalised and z again
+        feed.get(0, y);
         float2 yrstd = both(1.f);
         if (a.post != RTOSS_NORM_NONE) {
             if (a.post == RTOSS_NORM_LAYER) less_mean<VEC, G, P>(red, y, at, threads, D, inv_d);
@@ -479,71 +489,56 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
             red.template sum<1>(s);
             yrstd = both(rsqrtf(s[0] * inv_d + a.eps));
         }
+        feed.get(1, z);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            float2 w_[4], g_[4];
-            if (!kHold) weights(a.wpost, p, w_), gates(p, g_);
-            float2(&w)[4] = kHold ? wpost_[p] : w_;
-            float2(&g)[4] = kHold ? gate_[p] : g_;
+        for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 y[p][j] = mul2(y[p][j], yrstd);
-                z[p][j] = fma2(g[j], mul2(y[p][j], w[j]), mul2(scale, z[p][j]));
+                z[p][j] = fma2(gw[p][j], y[p][j], mul2(scale, z[p][j]));
             }
-        }
         if (a.pre != RTOSS_NORM_NONE) {
             if (a.pre == RTOSS_NORM_LAYER) less_mean<VEC, G, P>(red, z, at, threads, D, inv_d);
+            feed.get(3, dn);
             float2 q = both(0.f), b = both(0.f), c = both(0.f);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                float2 w_[4];
-                if (!kHold) weights(a.wpre, p, w_);
-                float2(&w)[4] = kHold ? wpre_[p] : w_;
+            for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float2 g = mul2(dn[p][j], w[j]);
+                    const float2 g = mul2(dn[p][j], wpre[p][j]);
                     q = fma2(z[p][j], z[p][j], q);
                     b = fma2(g, z[p][j], b);
                     c = add2(c, g);
                 }
-            }
             float s[3] = {q.x + q.y, b.x + b.y, c.x + c.y};
             red.template sum<3>(s);
             const float rstd = rsqrtf(s[0] * inv_d + a.eps);
             const float2 zrstd = both(rstd), m0 = both(-(s[1] * rstd) * inv_d);
             const float m1 = a.pre == RTOSS_NORM_LAYER ? -s[2] * inv_d : 0.f;
+            feed.get(2, dz);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                float2 w_[4];
-                if (!kHold) weights(a.wpre, p, w_);
-                float2(&w)[4] = kHold ? wpre_[p] : w_;
+            for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float2 hat = mul2(z[p][j], zrstd);
                     if (live) s_pre[p][j] = fma2(dn[p][j], hat, s_pre[p][j]);
-                    const float2 g = fma2(hat, m0, fma2(dn[p][j], w[j], inside<VEC>(m1, (p * threads + at) * 8 + 2 * j, D)));
+                    const float2 g = fma2(hat, m0, fma2(dn[p][j], wpre[p][j], inside<VEC>(m1, (p * threads + at) * 8, j, D)));
                     dz[p][j] = fma2(zrstd, g, dz[p][j]);
                 }
-            }
+        } else {
+            feed.get(2, dz);
         }
         // dz holds the whole gradient of z
         float2 b = both(0.f), c = both(0.f);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            float2 out[4], w_[4], g_[4];
-            if (!kHold) weights(a.wpost, p, w_), gates(p, g_);
-            float2(&w)[4] = kHold ? wpost_[p] : w_;
-            float2(&g)[4] = kHold ? gate_[p] : g_;
+            float2 out[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 out[j] = mul2(scale, dz[p][j]);
-                const float2 v = mul2(y[p][j], w[j]), dv = mul2(dz[p][j], g[j]);
-                if (live) {
-                    s_gate[p][j] = fma2(dz[p][j], v, s_gate[p][j]);
-                    s_post[p][j] = fma2(dv, y[p][j], s_post[p][j]);
-                }
-                b = fma2(dv, v, b);
-                dz[p][j] = mul2(dv, w[j]);
+                if (live) s_all[p][j] = fma2(dz[p][j], y[p][j], s_all[p][j]);
+                dz[p][j] = mul2(dz[p][j], gw[p][j]);
+                b = fma2(dz[p][j], y[p][j], b);
                 c = add2(c, dz[p][j]);
             }
             if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.dr, a.dr_ld, row, (p * threads + at) * 8, D, out);
@@ -556,26 +551,34 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dz[p][j] = mul2(yrstd, add2(fma2(y[p][j], m0, dz[p][j]), m1));
-        } else if (feed.RING && a.pre == RTOSS_NORM_NONE) {
+        } else if (feed.RING) {
             __syncthreads();   // (the stage is free)
         }
 #pragma unroll
         for (int p = 0; p < P; ++p)
             if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.dy, a.dy_ld, row, (p * threads + at) * 8, D, dz[p]);
         // a gate's last row here: its sum is final when all its rows were this unit's, else one of the unit's two shares
-        if (a.dgate && live && (row + 1 == row1 || row + 1 == gate_at)) {
+        if (live && (row + 1 == row1 || row + 1 == gate_at)) {
             const int first = gate_at - a.S;   // (S divides the tokens)
             const bool whole = first >= row0 && gate_at <= row1;
             float* part = a.p_gate + ((long long)unit * 2 + (first > row0 ? 1 : 0)) * D;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int i = (p * threads + at) * 8;
-                if (i < D) {
-                    if (whole) store8<T, VEC>(a.dgate, a.dgate_ld, gate_row, i, D, s_gate[p]);
-                    else store8<float, VEC>(part, 0, 0, i, D, s_gate[p]);
-                }
+                float2 w[4], g[4];
+                weights(a.wpost, p, w);
+                gates(p, g);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s_gate[p][j] = both(0.f);
+                for (int j = 0; j < 4; ++j) {
+                    float2& t = G <= 32 ? s_post[G <= 32 ? p : 0][j] : post_sum[p * threads * 4 + j];
+                    t = fma2(g[j], s_all[p][j], t);
+                    w[j] = mul2(w[j], s_all[p][j]);
+                    s_all[p][j] = both(0.f);
+                }
+                if (a.dgate && i < D) {
+                    if (whole) store8<T, VEC>(a.dgate, a.dgate_ld, gate_row, i, D, w);
+                    else store8<float, VEC>(part, 0, 0, i, D, w);
+                }
             }
         }
     }
@@ -602,7 +605,12 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
         for (int p = 0; p < P; ++p) {
             const int i = (p * threads + at) * 8;
             if (i >= D) continue;
-            if (a.p_post) store8<float, VEC>(a.p_post, D, unit, i, D, s_post[p]);
+            if (a.p_post) {
+                float2 v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = post_sum[p * threads * 4 + j];
+                store8<float, VEC>(a.p_post, D, unit, i, D, v);
+            }
             if (a.p_pre) store8<float, VEC>(a.p_pre, D, unit, i, D, s_pre[p]);
         }
     }
@@ -784,12 +792,13 @@ struct Plan {
 };
 Plan plan_of(int64_t rows, int D, int sms, bool backward) {
     Plan p;
-    const int pieces = (D + 7) / 8, room = backward ? 512 : 1024;
-    p.P = D <= 4096 ? 1 : D <= 8192 ? 2 : 0;
-    p.G = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : pieces <= 128 ? 128 : pieces <= 256 ? 256 : 512;
+    const int pieces = (D + 7) / 8;
+    p.P = D <= (backward ? 2048 : 4096) ? 1 : D <= 8192 ? 2 : 0;
+    const int each = p.P ? (pieces + p.P - 1) / p.P : 0;   // pieces of a thread's first round
+    p.G = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : each <= 128 ? 128 : each <= 256 ? 256 : 512;
     if (p.P == 0) p.G = p.threads = kLongThreads, p.blocks = backward ? 1 : 2;
-    else if (p.G <= 32) p.threads = 256, p.blocks = room / 256;
-    else p.threads = ((pieces + p.P - 1) / p.P + 31) / 32 * 32, p.blocks = (p.P == 2 ? 512 : room) / p.threads;
+    else if (p.G <= 32) p.threads = 256, p.blocks = backward ? 2 : 4;
+    else p.threads = (each + 31) / 32 * 32, p.blocks = (p.P == 2 ? 512 : backward ? 768 : 1024) / p.threads;
     const int per_block = p.P && p.G <= 32 ? 256 / p.G : 1;
     const int64_t most = (int64_t)sms * p.blocks * per_block;
     const int64_t units = rows < most ? rows : most;
@@ -806,13 +815,14 @@ int launch_one(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s)
         else return norm_forward_kernel<T, VEC, G, P>;
     }();
     int smem = 0;
-    if constexpr (VEC && G > 32) {
-        // an SM's 227 KB, less a kilobyte of the system's and one of a block's own
-        const int stage = a.D * (int)sizeof(T) * (BACKWARD ? 4 : 2), room = 227 * 1024 / p.blocks - 2 * 1024;
-        int n = room / stage;
-        n = n < kMaxStages ? n : kMaxStages;
-        a.stages = n < p.per_unit ? n : p.per_unit;
-        smem = a.stages * stage;
+    if constexpr (G > 32) {
+        if (BACKWARD) smem = p.threads * P * 32;   // sums for post_weight
+        if (VEC) {
+            // an SM's 227 KB, less a kilobyte of the system's and one of a block's own
+            const int stage = a.D * (int)sizeof(T) * (BACKWARD ? 4 : 2), n = (227 * 1024 / p.blocks - 2 * 1024 - smem) / stage;
+            a.stages = min(n < kMaxStages ? n : kMaxStages, p.per_unit);
+            smem += a.stages * stage;
+        }
         static std::atomic<bool> allowed[64];
         const int dev = ctx->device;
         if (smem > 40 * 1024 && (dev >= 64 || !allowed[dev].load(std::memory_order_acquire))) {
@@ -829,8 +839,12 @@ int launch_as(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s) 
     if (p.G == 16) return launch_one<T, VEC, 16, 1, BACKWARD>(ctx, p, a, s);
     if (p.G == 32) return launch_one<T, VEC, 32, 1, BACKWARD>(ctx, p, a, s);
     if (p.G == 128) return launch_one<T, VEC, 128, 1, BACKWARD>(ctx, p, a, s);
-    if (p.G == 256) return launch_one<T, VEC, 256, 1, BACKWARD>(ctx, p, a, s);
-    if (p.P == 1) return launch_one<T, VEC, 512, 1, BACKWARD>(ctx, p, a, s);
+    if (p.G == 256 && p.P == 1) return launch_one<T, VEC, 256, 1, BACKWARD>(ctx, p, a, s);
+    if constexpr (BACKWARD) {
+        if (p.G == 256) return launch_one<T, VEC, 256, 2, BACKWARD>(ctx, p, a, s);
+    } else {
+        if (p.P == 1) return launch_one<T, VEC, 512, 1, BACKWARD>(ctx, p, a, s);
+    }
     return launch_one<T, VEC, 512, 2, BACKWARD>(ctx, p, a, s);
 }
 
