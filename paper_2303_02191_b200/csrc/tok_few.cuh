@@ -18,7 +18,6 @@ namespace rtoss_tok {
 
 constexpr int kFewTokens = 16;
 constexpr int kFewWarps = 8;
-constexpr int kFewUnroll = 4;
 
 struct FewArgs {
     const void* x;
@@ -86,6 +85,9 @@ __device__ __forceinline__ void mma_few(unsigned (&c)[4], unsigned a0, unsigned 
 template <typename E, typename T, bool GATED, int NT>
 __global__ void __launch_bounds__(kFewWarps * 32) tok_few_kernel(const FewArgs a) {
     constexpr int kPer = 16 / (int)sizeof(E), kTok = 8 * NT;
+    // Groups of four pieces that a warp loads before it multiplies: two, so that more blocks fit an SM and none waits for long
+    // (one token, 2048 -> 5632: 15.0 us, with four 18.0); four for 9 to 16 tokens in 16 bits (1024 -> 2816: 7.9 us, with two 10.1).
+    constexpr int kUnroll = NT == 2 && sizeof(E) == 2 ? 4 : 2;
     __shared__ unsigned s_part[kFewWarps][16 * kTok];
     __shared__ unsigned s_sum[8][16 * kTok];   // of the blocks of the cluster (rank 0's copy is the one that counts)
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -98,43 +100,53 @@ __global__ void __launch_bounds__(kFewWarps * 32) tok_few_kernel(const FewArgs a
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const int r0 = GATED ? group * 8 : group * 16;
+    // (what rows behind the last one and tokens that are not there would add up to is not written: they read the first ones)
     const E* w0 = reinterpret_cast<const E*>(a.w0);
-    const E* rowA;
-    const E* rowB;
-    bool inA, inB;
-    if (GATED) {
-        inA = inB = r0 + g < a.rows;
-        rowA = w0 + (long long)(r0 + g) * a.w_ld;
-        rowB = reinterpret_cast<const E*>(a.w1) + (long long)(r0 + g) * a.w1_ld;
-    } else {
-        inA = r0 + g < a.rows;
-        inB = r0 + g + 8 < a.rows;
-        rowA = w0 + (long long)(r0 + g) * a.w_ld;
-        rowB = rowA + 8 * a.w_ld;
-    }
-    const E* x = reinterpret_cast<const E*>(a.x) + (long long)g * a.x_ld;
+    const E* rowA = w0 + (long long)(r0 + g < a.rows ? r0 + g : r0) * a.w_ld;
+    const E* rowB = GATED ? reinterpret_cast<const E*>(a.w1) + (long long)(r0 + g < a.rows ? r0 + g : r0) * a.w1_ld
+                          : w0 + (long long)(r0 + g + 8 < a.rows ? r0 + g + 8 : r0) * a.w_ld;
+    const E* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x[n] = reinterpret_cast<const E*>(a.x) + (8 * n + g < a.tokens ? (long long)(8 * n + g) * a.x_ld : 0ll);
     unsigned c[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) c[n][i] = 0u;
 
-    // pieces of 16 bytes: this block takes [first, last), a warp kFewUnroll groups of four at a time
+    // pieces of 16 bytes: this block takes [first, last), a warp kUnroll groups of four at a time
     const int pieces = (a.K + kPer - 1) / kPer, first = (int)rank * a.share, last = min(pieces, first + a.share);
-    for (int p0 = first + warp * 4 * kFewUnroll; p0 < last; p0 += kFewWarps * 4 * kFewUnroll) {
-        uint4 wa[kFewUnroll], wb[kFewUnroll], xb[kFewUnroll][NT];
+    // (loads without conditions, all in flight at once, but for the last round and rows whose end cuts a piece: with conditions
+    // the block of one token, 2048 -> 5632, took 27 us, without them 15)
+    const int all = min(last, a.K / kPer);
+    for (int p0 = first + warp * 4 * kUnroll; p0 < last; p0 += kFewWarps * 4 * kUnroll) {
+        uint4 wa[kUnroll], wb[kUnroll], xb[kUnroll][NT];
+        if (p0 + 4 * kUnroll <= all) {
 #pragma unroll
-        for (int u = 0; u < kFewUnroll; ++u) {
-            const int p = p0 + 4 * u + t, k = p * kPer;
-            const bool in = p < last;
-            wa[u] = in && inA ? row_piece(rowA, k, a.K) : make_uint4(0u, 0u, 0u, 0u);
-            wb[u] = in && inB ? row_piece(rowB, k, a.K) : make_uint4(0u, 0u, 0u, 0u);
+            for (int u = 0; u < kUnroll; ++u) {
+                const int k = (p0 + 4 * u + t) * kPer;
+                wa[u] = *reinterpret_cast<const uint4*>(rowA + k);
+                wb[u] = *reinterpret_cast<const uint4*>(rowB + k);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-                xb[u][n] = in && 8 * n + g < a.tokens ? row_piece(x + (long long)(8 * n) * a.x_ld, k, a.K) : make_uint4(0u, 0u, 0u, 0u);
+                for (int n = 0; n < NT; ++n) xb[u][n] = *reinterpret_cast<const uint4*>(x[n] + k);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int p = p0 + 4 * u + t;
+                wa[u] = wb[u] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) xb[u][n] = make_uint4(0u, 0u, 0u, 0u);
+                if (p < last) {
+                    wa[u] = row_piece(rowA, p * kPer, a.K);
+                    wb[u] = row_piece(rowB, p * kPer, a.K);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) xb[u][n] = row_piece(x[n], p * kPer, a.K);
+                }
+            }
         }
 #pragma unroll
-        for (int u = 0; u < kFewUnroll; ++u)
+        for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 mma_few<E>(c[n], wa[u].x, wb[u].x, wa[u].y, wb[u].y, xb[u][n].x, xb[u][n].y);
@@ -211,11 +223,11 @@ int launch_few(const rtoss_ctx* ctx, FewArgs& a, cudaStream_t stream) {
     const int groups = (a.rows + per - 1) / per, pieces = (a.K + 16 / (int)sizeof(E) - 1) / (16 / (int)sizeof(E));
     // as many blocks to a cluster as it takes to have two blocks an SM, while each still has work for its warps
     int ranks = 1;
-    while (ranks < 8 && groups * ranks < 2 * sms && pieces / (2 * ranks) >= kFewWarps * 4 * kFewUnroll / 2) ranks *= 2;
+    while (ranks < 8 && groups * ranks < 2 * sms && pieces / (2 * ranks) >= kFewWarps * 4) ranks *= 2;
     a.share = ((pieces + ranks - 1) / ranks + 3) / 4 * 4;
     const dim3 grid((unsigned)(groups * ranks));
-    return a.tokens <= 8 ? (int)rtoss_dev::launch_pdl(tok_few_kernel<E, T, GATED, 1>, grid, dim3(kFewWarps * 32), 0, stream, ranks, a)
-                         : (int)rtoss_dev::launch_pdl(tok_few_kernel<E, T, GATED, 2>, grid, dim3(kFewWarps * 32), 0, stream, ranks, a);
+    auto go = [&](auto kernel) { return (int)rtoss_dev::launch_pdl(kernel, grid, dim3(kFewWarps * 32), 0, stream, ranks, a); };
+    return a.tokens <= 8 ? go(tok_few_kernel<E, T, GATED, 1>) : go(tok_few_kernel<E, T, GATED, 2>);
 }
 
 }  // namespace rtoss_tok
