@@ -374,15 +374,16 @@ def _bad(what, why):
     raise RtossError(ERR_INVALID_ARG, "%s: %s" % (what, why))
 
 
-def _matrix(t, rows, cols, dtype, device, what):
-    """(address, row stride) of a CUDA matrix [rows, cols] whose values of a row are neighbours; (0, 0) for None."""
+def _matrix(t, shape, dtype, device, what):
+    """(address, row stride) of a CUDA matrix of that shape whose values of a row are neighbours; (0, 0) for None."""
     if t is None:
         return 0, 0
-    if t.dtype is not dtype or t.dim() != 2 or t.size(0) != rows or t.size(1) != cols:
-        _bad(what, "need %s [%d, %d], got %s %s" % (dtype, rows, cols, t.dtype, list(t.shape)))
+    if t.shape != shape or t.dtype is not dtype:
+        _bad(what, "need %s %s, got %s %s" % (dtype, list(shape), t.dtype, list(t.shape)))
     if t.get_device() != device:
         _bad(what, "is not on the context's device")
     step, inner = t.stride()
+    rows, cols = shape
     if inner != 1 and cols > 1:
         _bad(what, "the values of a row must be neighbours in memory")
     if rows <= 1:
@@ -392,15 +393,25 @@ def _matrix(t, rows, cols, dtype, device, what):
     return t.data_ptr(), step
 
 
-def _vector(t, n, dtype, device, what):
-    """Address of a contiguous CUDA vector [n]; 0 for None."""
+def _vector(t, shape, dtype, device, what):
+    """Address of a contiguous CUDA vector of that shape; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
-        _bad(what, "need contiguous %s [%d], got %s %s" % (dtype, n, t.dtype, list(t.shape)))
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        _bad(what, "need contiguous %s %s, got %s %s" % (dtype, list(shape), t.dtype, list(t.shape)))
     if t.get_device() != device:
         _bad(what, "is not on the context's device")
     return t.data_ptr()
+
+
+_F32 = _I8 = None
+
+
+def _types():
+    """torch's types, looked up once (an import statement in every call costs a tenth of a small call)."""
+    global _F32, _I8
+    import torch
+    _F32, _I8 = torch.float32, torch.int8
 
 
 class Context:
@@ -573,25 +584,28 @@ class Context:
     # -- operators over tokens (matrices are 2-D CUDA tensors; column slices are fine) ------------------------------------
     def rtoss_quantize_rows(self, x, q, scale):
         """x [rows, cols] fp32 / bf16 / fp16 -> int8 codes q [rows, cols] and fp32 scale [rows]."""
-        import torch
-        rows, cols = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
-        xp, xs = _matrix(x, rows, cols, x.dtype, self.device, "x")
-        qp, qs = _matrix(q, rows, cols, torch.int8, self.device, "q")
+        if _F32 is None:
+            _types()
+        shape = rows, cols = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
+        xp, xs = _matrix(x, shape, x.dtype, self.device, "x")
+        qp, qs = _matrix(q, shape, _I8, self.device, "q")
         st = lib.rtoss_quantize_rows(self.h, xp, _torch_dtype_code(x), rows, cols, xs, qp, qs,
-                                     _vector(scale, rows, torch.float32, self.device, "scale"), _stream_on(self.device))
+                                     _vector(scale, (rows,), _F32, self.device, "scale"), _stream_on(self.device))
         if st:
             self._check(st)
         return q, scale
 
     def rtoss_matmul_i8(self, x, x_scale, w, w_scale, y, act=ACT_NONE, bias=None, residual=None, residual_after_act=False):
         """y [tokens, N] = act(x_scale * w_scale * (x [tokens, K] @ w [N, K]^T) + bias + residual)."""
-        import torch
+        if _F32 is None:
+            _types()
         tokens, K = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
-        N, d, f32 = w.size(0), self.device, torch.float32
+        N, d, t = w.size(0) if w.dim() == 2 else _bad("w", "need a matrix"), self.device, y.dtype
+        out, each = (tokens, N), (N,)
         st = lib.rtoss_matmul_i8(self.h, _I8_PRODUCT.pack(
-            tokens, K, N, *_matrix(x, tokens, K, torch.int8, d, "x"), *_matrix(w, N, K, torch.int8, d, "w"),
-            *_matrix(y, tokens, N, y.dtype, d, "y"), *_matrix(residual, tokens, N, y.dtype, d, "residual"),
-            _vector(x_scale, tokens, f32, d, "x_scale"), _vector(w_scale, N, f32, d, "w_scale"), _vector(bias, N, f32, d, "bias"),
+            tokens, K, N, *_matrix(x, (tokens, K), _I8, d, "x"), *_matrix(w, (N, K), _I8, d, "w"),
+            *_matrix(y, out, t, d, "y"), *_matrix(residual, out, t, d, "residual"),
+            _vector(x_scale, (tokens,), _F32, d, "x_scale"), _vector(w_scale, each, _F32, d, "w_scale"), _vector(bias, each, _F32, d, "bias"),
             _torch_dtype_code(y), act, 1 if residual_after_act else 0), _stream_on(d))
         if st:
             self._check(st)
@@ -601,11 +615,12 @@ class Context:
         """h [tokens, F] = act(x w_gate^T) * (x w_up^T), y [tokens, D] = h w_down^T; gate, up: kept for the backward pass.
         w_down and y may be None together.  Returns y, or h."""
         tokens, D = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
-        F, t, d = w_gate.size(0), x.dtype, self.device
+        F, t, d = w_gate.size(0) if w_gate.dim() == 2 else _bad("w_gate", "need a matrix"), x.dtype, self.device
+        row, mid, win, wout = (tokens, D), (tokens, F), (F, D), (D, F)
         st = lib.rtoss_gated_ffn_forward(self.h, _FFN.pack(
-            tokens, D, F, _torch_dtype_code(x), act, *_matrix(x, tokens, D, t, d, "x"), *_matrix(w_gate, F, D, t, d, "w_gate"),
-            *_matrix(w_up, F, D, t, d, "w_up"), *_matrix(w_down, D, F, t, d, "w_down"), *_matrix(h, tokens, F, t, d, "h"),
-            *_matrix(gate, tokens, F, t, d, "gate"), *_matrix(up, tokens, F, t, d, "up"), *_matrix(y, tokens, D, t, d, "y"),
+            tokens, D, F, _torch_dtype_code(x), act, *_matrix(x, row, t, d, "x"), *_matrix(w_gate, win, t, d, "w_gate"),
+            *_matrix(w_up, win, t, d, "w_up"), *_matrix(w_down, wout, t, d, "w_down"), *_matrix(h, mid, t, d, "h"),
+            *_matrix(gate, mid, t, d, "gate"), *_matrix(up, mid, t, d, "up"), *_matrix(y, row, t, d, "y"),
             0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
         if st:
             self._check(st)
@@ -617,13 +632,14 @@ class Context:
         that are given; h, dgate, dup [tokens, F] are workspaces (dgate may be gate and dup up)."""
         tokens, D = dy.shape if dy.dim() == 2 else _bad("dy", "need a matrix")
         F, t, d = w_down.size(1) if w_down.dim() == 2 else _bad("w_down", "need a matrix"), dy.dtype, self.device
+        row, mid, win, wout = (tokens, D), (tokens, F), (F, D), (D, F)
         st = lib.rtoss_gated_ffn_backward(self.h, _FFN.pack(
-            tokens, D, F, _torch_dtype_code(dy), act, *_matrix(x, tokens, D, t, d, "x"), *_matrix(w_gate, F, D, t, d, "w_gate"),
-            *_matrix(w_up, F, D, t, d, "w_up"), *_matrix(w_down, D, F, t, d, "w_down"), *_matrix(h, tokens, F, t, d, "h"),
-            *_matrix(gate, tokens, F, t, d, "gate"), *_matrix(up, tokens, F, t, d, "up"), 0, 0, *_matrix(dy, tokens, D, t, d, "dy"),
-            *_matrix(dgate, tokens, F, t, d, "dgate"), *_matrix(dup, tokens, F, t, d, "dup"), *_matrix(dx, tokens, D, t, d, "dx"),
-            *_matrix(dw_gate, F, D, t, d, "dw_gate"), *_matrix(dw_up, F, D, t, d, "dw_up"),
-            *_matrix(dw_down, D, F, t, d, "dw_down")), _stream_on(d))
+            tokens, D, F, _torch_dtype_code(dy), act, *_matrix(x, row, t, d, "x"), *_matrix(w_gate, win, t, d, "w_gate"),
+            *_matrix(w_up, win, t, d, "w_up"), *_matrix(w_down, wout, t, d, "w_down"), *_matrix(h, mid, t, d, "h"),
+            *_matrix(gate, mid, t, d, "gate"), *_matrix(up, mid, t, d, "up"), 0, 0, *_matrix(dy, row, t, d, "dy"),
+            *_matrix(dgate, mid, t, d, "dgate"), *_matrix(dup, mid, t, d, "dup"), *_matrix(dx, row, t, d, "dx"),
+            *_matrix(dw_gate, win, t, d, "dw_gate"), *_matrix(dw_up, win, t, d, "dw_up"),
+            *_matrix(dw_down, wout, t, d, "dw_down")), _stream_on(d))
         if st:
             self._check(st)
         return dx, dw_gate, dw_up, dw_down
@@ -632,15 +648,16 @@ class Context:
                                  tokens_per_gate=0, residual_scale=1.0, eps=1e-6):
         """z = residual_scale * r + gate * norm_post(y), n = norm_pre(z); gate [tokens / tokens_per_gate, D] (0: all tokens
         share one).  Returns (z, n)."""
-        import torch
-        tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
-        t, d, f32 = y.dtype, self.device, torch.float32
+        if _F32 is None:
+            _types()
+        row = tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
+        t, d, each = y.dtype, self.device, (D,)
         share = tokens_per_gate or max(tokens, 1)
         st = lib.rtoss_block_norm_forward(self.h, _BLOCK_NORM.pack(
-            tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, D, f32, d, "post_weight"),
-            _vector(pre_weight, D, f32, d, "pre_weight"), *_matrix(r, tokens, D, t, d, "r"), *_matrix(y, tokens, D, t, d, "y"),
-            *_matrix(gate, max(tokens // share, 1), D, t, d, "gate"), *_matrix(z, tokens, D, t, d, "z"),
-            *_matrix(n, tokens, D, t, d, "n"), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
+            tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, each, _F32, d, "post_weight"),
+            _vector(pre_weight, each, _F32, d, "pre_weight"), *_matrix(r, row, t, d, "r"), *_matrix(y, row, t, d, "y"),
+            *_matrix(gate, (max(tokens // share, 1), D), t, d, "gate"), *_matrix(z, row, t, d, "z"),
+            *_matrix(n, row, t, d, "n"), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
         if st:
             self._check(st)
         return z, n
@@ -657,19 +674,20 @@ class Context:
                                   dgate=None, workspace=None):
         """Gradients dr, dy, dpost_weight, dpre_weight (fp32 [D]) and dgate of rtoss_block_norm_forward from dz and dn (either
         may be None)."""
-        import torch
-        tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
-        t, d, f32 = y.dtype, self.device, torch.float32
+        if _F32 is None:
+            _types()
+        row = tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
+        t, d, each = y.dtype, self.device, (D,)
         share = tokens_per_gate or max(tokens, 1)
-        gates = max(tokens // share, 1)
+        gates = (max(tokens // share, 1), D)
         floats = 0 if workspace is None else workspace.numel()
         st = lib.rtoss_block_norm_backward(self.h, _BLOCK_NORM.pack(
-            tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, D, f32, d, "post_weight"),
-            _vector(pre_weight, D, f32, d, "pre_weight"), *_matrix(r, tokens, D, t, d, "r"), *_matrix(y, tokens, D, t, d, "y"),
-            *_matrix(gate, gates, D, t, d, "gate"), 0, 0, 0, 0, *_matrix(dz, tokens, D, t, d, "dz"), *_matrix(dn, tokens, D, t, d, "dn"),
-            *_matrix(dr, tokens, D, t, d, "dr"), *_matrix(dy, tokens, D, t, d, "dy"), *_matrix(dgate, gates, D, t, d, "dgate"),
-            _vector(dpost_weight, D, f32, d, "dpost_weight"), _vector(dpre_weight, D, f32, d, "dpre_weight"),
-            _vector(workspace, floats, f32, d, "workspace"), floats), _stream_on(d))
+            tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, each, _F32, d, "post_weight"),
+            _vector(pre_weight, each, _F32, d, "pre_weight"), *_matrix(r, row, t, d, "r"), *_matrix(y, row, t, d, "y"),
+            *_matrix(gate, gates, t, d, "gate"), 0, 0, 0, 0, *_matrix(dz, row, t, d, "dz"), *_matrix(dn, row, t, d, "dn"),
+            *_matrix(dr, row, t, d, "dr"), *_matrix(dy, row, t, d, "dy"), *_matrix(dgate, gates, t, d, "dgate"),
+            _vector(dpost_weight, each, _F32, d, "dpost_weight"), _vector(dpre_weight, each, _F32, d, "dpre_weight"),
+            _vector(workspace, (floats,), _F32, d, "workspace"), floats), _stream_on(d))
         if st:
             self._check(st)
         return dr, dy

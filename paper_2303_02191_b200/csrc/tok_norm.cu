@@ -39,7 +39,7 @@ struct NormArgs {
     int stages;        // rows that the ring of a block holds (RowFeed)
     int* status;
     long long wait;    // limit of a wait, in clocks
-    float *p_post, *p_pre, *p_gate;   // partial sums: [block][D], [block][D], [unit][2][D]
+    float *p_post, *p_pre, *p_gate;   // partial sums: [block][D], [block][D], [block][2][D]
     void* dgate;
 };
 
@@ -436,7 +436,9 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
     feed.ld[0] = a.y_ld, feed.ld[1] = a.r_ld, feed.ld[2] = a.dz_ld, feed.ld[3] = a.dn_ld;
     feed.start();
     float2 gw[P][4], wpre[P][4], s_all[P][4], s_pre[P][4], s_post[G <= 32 ? P : 1][4];
-    // (G > 32: the sums for post_weight lie behind the ring, a thread's own columns)
+    // (G > 32: the sums for post_weight lie behind the ring, a thread's own columns; else: what a unit has of its first and its last
+    // gate, where others have the rest)
+    __shared__ float2 share[G <= 32 ? 2 : 1][G <= 32 ? 256 : 1][4];
     float2* const post_sum = reinterpret_cast<float2*>(ring + (feed.RING ? a.stages * 4 * D * (int)sizeof(T) : 0)) + at * 4;
     auto weights = [&](const float* w, int p, float2 (&v)[4]) {
         const int i = (p * threads + at) * 8;
@@ -557,11 +559,11 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
 #pragma unroll
         for (int p = 0; p < P; ++p)
             if ((p * threads + at) * 8 < D && live) store8<T, VEC>(a.dy, a.dy_ld, row, (p * threads + at) * 8, D, dz[p]);
-        // a gate's last row here: its sum is final when all its rows were this unit's, else one of the unit's two shares
+        // a gate's last row here: its sum is final when all its rows were this unit's, else one of the unit's (or block's) two shares
         if (live && (row + 1 == row1 || row + 1 == gate_at)) {
             const int first = gate_at - a.S;   // (S divides the tokens)
             const bool whole = first >= row0 && gate_at <= row1;
-            float* part = a.p_gate + ((long long)unit * 2 + (first > row0 ? 1 : 0)) * D;
+            float* part = a.p_gate + ((long long)blockIdx.x * 2 + (first > row0 ? 1 : 0)) * D;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int i = (p * threads + at) * 8;
@@ -577,12 +579,42 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_b
                 }
                 if (a.dgate && i < D) {
                     if (whole) store8<T, VEC>(a.dgate, a.dgate_ld, gate_row, i, D, w);
-                    else store8<float, VEC>(part, 0, 0, i, D, w);
+                    else if constexpr (G > 32) store8<float, VEC>(part, 0, 0, i, D, w);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) share[first > row0][threadIdx.x][j] = w[j];
                 }
             }
         }
     }
     if constexpr (G <= 32) {
+        if (a.dgate) {
+            // Gates of several units: the first unit of the block that meets one adds the shares in the units' order.  The sum is final
+            // when all rows were this block's, else one of the block's two shares.
+            __syncthreads();
+            constexpr int U = 256 / G;
+            const int u0 = (int)threadIdx.x / G, i = at * 8;
+            const long long b0 = (long long)blockIdx.x * U * a.per_unit, b1 = min((long long)a.rows, b0 + (long long)U * a.per_unit);
+            auto join = [&](int gr) {
+                const long long first = (long long)gr * a.S, last = first + a.S;
+                if ((first >= row0 && last <= row1) || (first < row0 && u0 > 0)) return;   // written already, or another unit's to add
+                float2 t[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
+                for (int u = u0; u < U; ++u) {
+                    const long long r = b0 + (long long)u * a.per_unit;
+                    if (r >= last || r >= b1) break;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) t[j] = add2(t[j], share[first > r][u * G + at][j]);
+                }
+                if (i >= D) return;
+                if (first >= b0 && last <= b1) store8<T, VEC>(a.dgate, a.dgate_ld, gr, i, D, t);
+                else store8<float, VEC>(a.p_gate + ((long long)blockIdx.x * 2 + (first > b0 ? 1 : 0)) * D, 0, 0, i, D, t);
+            };
+            if (row0 < row1) {
+                const int head = row0 / a.S, tail = (row1 - 1) / a.S;
+                join(head);
+                if (tail != head) join(tail);
+            }
+        }
         // the block's units, added in their order
         __shared__ float2 part[256][4];
 #pragma unroll
@@ -730,10 +762,10 @@ struct JoinArgs {
     float *dpost, *dpre;
     void* dgate;
     long long dgate_ld;
-    int D, parts, per_unit, S, by_gate;   // parts: rows of p_post and p_pre
+    int D, parts, per_part, S, by_gate;   // parts: blocks that left sums; per_part: rows of one
 };
 
-// 32 threads with four columns each a block, 32 runs of units side by side, joined in their order.
+// 32 threads with four columns each a block, 32 runs of partial sums side by side, joined in their order.
 constexpr int kJoinRuns = 32;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArgs a) {
@@ -745,12 +777,12 @@ __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArg
     long long pitch = a.D;
     long long row0 = 0;   // first row of the gate
     if (what >= 2) {
-        // gates that run across the end of a unit (the others are written already), counted by gate or, where there are fewer
-        // of them, by the unit whose end is a gate's first such end
-        const long long end = (long long)(what - 1) * a.per_unit;
+        // gates that run across the end of a block's rows (the others are written already), counted by gate or, where there are fewer
+        // of them, by the block whose end is a gate's first such end
+        const long long end = (long long)(what - 1) * a.per_part;
         row0 = a.by_gate ? (long long)(what - 2) * a.S : end / a.S * a.S;
-        first = (int)(row0 / a.per_unit);
-        last = (int)((row0 + a.S - 1) / a.per_unit) + 1;
+        first = (int)(row0 / a.per_part);
+        last = (int)((row0 + a.S - 1) / a.per_part) + 1;
         if (last - first == 1 || (!a.by_gate && (row0 == end || first != what - 2))) return;
         p = a.p_gate;
         pitch = 2ll * a.D;
@@ -763,8 +795,8 @@ __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArg
     if (col < a.D) {
 #pragma unroll 5
         for (int u = lo; u < hi; ++u) {
-            // (a gate that begins inside a unit is that unit's second share)
-            const long long second = what >= 2 && row0 > (long long)u * a.per_unit ? a.D : 0;
+            // (a gate that begins inside a block's rows is that block's second share)
+            const long long second = what >= 2 && row0 > (long long)u * a.per_part ? a.D : 0;
             const float* at = p + u * pitch + second + col;
             if (VEC) add(*reinterpret_cast<const float4*>(at));
             else add(make_float4(at[0], col + 1 < a.D ? at[1] : 0.f, col + 2 < a.D ? at[2] : 0.f, col + 3 < a.D ? at[3] : 0.f));
@@ -787,8 +819,9 @@ __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArg
 // ---- host -------------------------------------------------------------------------------------------------------------------
 // How rows are dealt out: threads of a unit by the row's length, units by what the device holds at once.
 struct Plan {
-    int G, P, threads, blocks, units, per_unit;   // threads: of a block; blocks: of an SM
-    int parts;                                    // rows of partial sums: one a block
+    int G, P, threads, blocks, per_unit;   // threads: of a block; blocks: of an SM; per_unit: rows of a unit
+    int parts, per_part;                   // blocks, each with a row of partial sums; rows of one
+    int room;                              // partial sums that a workspace has room for
 };
 Plan plan_of(int64_t rows, int D, int sms, bool backward) {
     Plan p;
@@ -800,11 +833,11 @@ Plan plan_of(int64_t rows, int D, int sms, bool backward) {
     else if (p.G <= 32) p.threads = 256, p.blocks = backward ? 2 : 4;
     else p.threads = (each + 31) / 32 * 32, p.blocks = (p.P == 2 ? 512 : backward ? 768 : 1024) / p.threads;
     const int per_block = p.P && p.G <= 32 ? 256 / p.G : 1;
-    const int64_t most = (int64_t)sms * p.blocks * per_block;
-    const int64_t units = rows < most ? rows : most;
+    const int64_t most = (int64_t)sms * p.blocks * per_block, units = rows < most ? rows : most;
     p.per_unit = (int)((rows + units - 1) / units);
-    p.units = (int)((rows + p.per_unit - 1) / p.per_unit);
-    p.parts = (p.units + per_block - 1) / per_block;
+    p.per_part = p.per_unit * per_block;
+    p.parts = (int)((rows + p.per_part - 1) / p.per_part);
+    p.room = (int)(rows < (int64_t)sms * p.blocks ? rows : (int64_t)sms * p.blocks);
     return p;
 }
 
@@ -855,7 +888,7 @@ int launch(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s) {
 }
 
 bool norm_ok(int k) { return k == RTOSS_NORM_NONE || k == RTOSS_NORM_RMS || k == RTOSS_NORM_LAYER; }
-int64_t ws_floats(const Plan& p, int D, bool gated) { return 2ll * p.parts * D + (gated ? 2ll * p.units * D : 0); }
+int64_t ws_floats(const Plan& p, int D, bool gated) { return (int64_t)p.room * D * (gated ? 4 : 2); }
 
 rtoss_status check(rtoss_ctx* ctx, const rtoss_block_norm* b, bool backward, const char* where) {
     if (!ctx) return RTOSS_ERR_INVALID_ARG;
@@ -915,11 +948,11 @@ int backward(const rtoss_ctx* ctx, const rtoss_block_norm* b, const Plan& p, cud
     a.p_pre = b->dpre_weight_dev ? ws + part : nullptr;
     a.p_gate = b->dgate.dev ? ws + 2 * part : nullptr;
     if (const int e = launch<T, true>(ctx, p, a, s)) return e;
-    const bool join_gates = a.dgate && p.units > 1 && p.per_unit % a.S != 0;   // (else every gate's rows were one unit's)
+    const bool join_gates = a.dgate && p.parts > 1 && p.per_part % a.S != 0;   // (else every gate's rows were one block's)
     if (!a.p_post && !a.p_pre && !join_gates) return 0;
-    const int gates = (int)(b->tokens / a.S), by_gate = gates < p.units;
-    JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.parts, p.per_unit, a.S, by_gate};
-    const dim3 grid((unsigned)((b->D + 127) / 128), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.units - 1)));
+    const int gates = (int)(b->tokens / a.S), by_gate = gates < p.parts;
+    JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.parts, p.per_part, a.S, by_gate};
+    const dim3 grid((unsigned)((b->D + 127) / 128), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.parts - 1)));
     return b->D % 4 == 0 ? (int)rtoss_dev::launch_pdl(norm_join_kernel<T, true>, grid, dim3(kJoinRuns * 32), 0, s, j)
                          : (int)rtoss_dev::launch_pdl(norm_join_kernel<T, false>, grid, dim3(kJoinRuns * 32), 0, s, j);
 }
