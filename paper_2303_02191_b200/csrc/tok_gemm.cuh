@@ -17,8 +17,9 @@
 //     into shared memory and leave the rest to TMA stores, which also cut off what lies outside the matrix.
 //   * CTA pairs are persistent and walk the tiles of up to three products (the weight gradients of the block) in groups of
 //     eight row tiles, so that the tiles in flight share their operands in L2.
-//   * Products with few tiles are cut along k: the pairs of a cluster of 2 KS CTAs take a share of k each, and exchange their
-//     fp32 sums through distributed shared memory; the shares are added in a fixed order.
+//   * Products with few tiles are cut along k: the pairs of a cluster of 2 KS CTAs take a share of k each, and send their sums to
+//     the pair that finishes a piece of the tile (st.async into its shared memory, counted by a barrier there; with barriers of
+//     the whole cluster on both sides the exchange took 8000 clocks, so EXCH).  The order of adding is fixed.
 //   * Every wait is bounded; one that runs out leaves a code in the context's status word and the CTA goes through the normal
 //     exit (TMEM is always released).
 #ifndef RTOSS_TOK_GEMM_CUH
@@ -58,6 +59,7 @@ template <int NP>
 struct GemmArgs {
     GemmProblem p[NP];
     int n_problems, tiles, KS;
+    int stages;                     // of the operand ring (the exchange of a split tile takes the place of some)
     int a_mn, b_mn;                 // operand lies with k across its rows
     unsigned idesc;
     int act;
@@ -95,8 +97,10 @@ struct GemmShape {
     static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 512;
     static constexpr int kTileN = MODE == kGated ? BN / 2 : BN;                    // output columns of a tile
     static constexpr int kTmemCols = 2 * BN;
-    // the exchange of a split tile lies in the operand ring
-    static_assert(BN * 128 * 4 <= kStages * kStageBytes, "no room for the exchange");
+    // Stages that KS pairs leave of the ring beside what each receives: the sums of KS - 1 others for its BN / KS columns.
+    static constexpr int stages_of(int KS) {
+        return KS == 1 ? kStages : kStages - (128 * (BN / KS) * (KS - 1) * 4 + kStageBytes - 1) / kStageBytes;
+    }
     static_assert(kSmem <= 227 * 1024, "shared memory");
     static_assert(kTmemCols <= 512, "TMEM");
 };
@@ -208,8 +212,10 @@ __device__ __forceinline__ void tmem_ld32(unsigned at, unsigned* r) {
 __device__ __forceinline__ void st_shared16(unsigned at, unsigned a, unsigned b, unsigned c, unsigned d) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void st_cluster16(unsigned at, unsigned a, unsigned b, unsigned c, unsigned d) {
-    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+// (bar: of the CTA that `at` lies in, which counts the bytes)
+__device__ __forceinline__ void send16(unsigned at, unsigned bar, unsigned a, unsigned b, unsigned c, unsigned d) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(at), "r"(bar), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
 }
 __device__ __forceinline__ uint4 ld_shared16(unsigned at) {
     uint4 v;
@@ -318,10 +324,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
     extern __shared__ unsigned char smem_raw[];
     const unsigned raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const unsigned s_stage = base, s_out = base + S::kStages * S::kStageBytes, s_bar = s_out + kEpiWarps * S::kStagingBytes;
-    const unsigned b_full = s_bar, b_empty = s_bar + 64, b_acc_full = s_bar + 128, b_acc_empty = s_bar + 144, s_tmem = s_bar + 160, b_edge = s_bar + 176;
+    const unsigned b_full = s_bar, b_empty = s_bar + 64, b_acc_full = s_bar + 128, b_acc_empty = s_bar + 144, s_tmem = s_bar + 160, b_edge = s_bar + 176, b_sums = s_bar + 304;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const unsigned rank = cta_rank(), half = rank & 1u, lead_rank = rank & ~1u, share = rank >> 1;
-    const int KS = g.KS;
+    const int KS = g.KS, stages = g.stages;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 0 && lane < 7) {
@@ -340,6 +346,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
         }
         if (MODE == kGateGrad)
             for (int i = 0; i < 2 * kEpiWarps; ++i) bar_init(b_edge + 8 * i, 1);
+        if (KS > 1) {
+            bar_init(b_sums, 1);
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b_sums), "r"(128 * (BN / KS) * (KS - 1) * 4) : "memory");
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -407,7 +417,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                     } else {
                         load_box(sb, mb, k0, n0, bar);
                     }
-                    if (++s == S::kStages) s = 0, ph ^= 1u;
+                    if (++s == stages) s = 0, ph ^= 1u;
                 }
             }
             if (!ok) {
@@ -441,7 +451,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                         add = 1;
                     }
                     commit_pair(leader, b_empty + 8 * s, mask);
-                    if (++s == S::kStages) s = 0, ph ^= 1u;
+                    if (++s == stages) s = 0, ph ^= 1u;
                 }
                 if (!ok) break;
                 commit_pair(leader, b_acc_full + 8 * as, mask);
@@ -622,7 +632,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                     // would wait for the stores on their way, 3000 clocks.
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0)
+                    if (lane == 0 && t + 2 * clusters < g.tiles)   // (else nothing waits for it)
                         asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(b_acc_empty + 8 * as, lead_rank)) : "memory");
                 }
                 ok = finish(at, col0 + u * S::kUnitCols, std::integral_constant<int, S::kUnitCols>(), acc, e, rs, cb) && ok;
@@ -636,38 +646,35 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             if (!as) aph ^= 1u;
         }
     }
-    if (KS > 1) {
-        // One tile a cluster.  Behind the first barrier every pair's products are complete, so the operand rings are free and
-        // take the other pairs' sums: of the tile's kShares pieces, the next kShares / KS belong to each pair.
+    if (KS > 1 && warp >= 4) {
+        // One tile a cluster.  Of the tile's kShares pieces, the next kShares / KS belong to each pair.
         const Tile at = tile_of(cluster);
-        if (warp >= 4) {
-            ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full, 0, g.wait));
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        }
-        __syncthreads();
-        cluster_barrier();
         constexpr int kAcc = S::kShareAcc;
         constexpr unsigned kSlot = 32 * kAcc * 4;   // a warp's sums of a piece
         const int per = S::kShares / KS;
-        auto slot = [&](int u, unsigned from) { return s_stage + ((unsigned)((u % per) * KS + (int)from) * 4u + (unsigned)quad) * kSlot + (unsigned)lane * 16u; };
-        if (warp >= 4 && ok) {
+        // where pair `to` keeps what pair `from` sends of piece u
+        auto slot = [&](int u, unsigned from, unsigned to) {
+            return s_stage + (unsigned)(stages * S::kStageBytes) + ((unsigned)((u % per) * (KS - 1)) + (from < to ? from : from - 1)) * (4u * kSlot) + (unsigned)quad * kSlot +
+                   (unsigned)lane * 16u;
+        };
+        ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full, 0, g.wait));
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (ok) {
 #pragma unroll 1
-            for (int u = side; u < S::kShares; u += 2) {
+            for (int v = side; v < S::kShares; v += 2) {
+                const int u = (v + (int)share * per) % S::kShares;   // (each pair begins with a piece of its own, then they go round)
                 const unsigned owner = (unsigned)(u / per);
                 if (owner == share) continue;
                 unsigned acc[kAcc];
                 read_acc(acc_at(0, u, kAcc), kAcc, acc);
                 loaded();
-                const unsigned to = at_rank(slot(u, share), 2 * owner + half);
+                const unsigned to = at_rank(slot(u, share, owner), 2 * owner + half), bar = at_rank(b_sums, 2 * owner + half);
 #pragma unroll
-                for (int j = 0; j < kAcc / 4; ++j) st_cluster16(to + j * 512, acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+                for (int j = 0; j < kAcc / 4; ++j) send16(to + j * 512, bar, acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
             }
-        }
-        __syncthreads();
-        cluster_barrier();
-        if (warp >= 4 && ok) {
+            bool here = false;
 #pragma unroll 1
-            for (int u = (int)share * per + (per > 1 ? side : 0); u < ((int)share + 1) * per; u += per > 1 ? 2 : 1) {
+            for (int u = (int)share * per + (per > 1 ? side : 0); u < ((int)share + 1) * per && ok; u += per > 1 ? 2 : 1) {
                 if (per == 1 && side != 0) break;
                 const int col = at.nt * S::kTileN + u * 32;
                 uint4 e[8];
@@ -676,50 +683,49 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                 const float rs = row_scale_of(at);
                 const float2 cb = column_of(at, col);
                 unsigned sum[kAcc];
-                // shares are added in their order, whichever pair adds them
-#pragma unroll
-                for (int j = 0; j < kAcc; ++j) sum[j] = 0u;
+                read_acc(acc_at(0, u, kAcc), kAcc, sum);   // this pair's own, then the others' in their order
+                loaded();
+                if (!here && !(ok = __all_sync(0xFFFFFFFFu, bar_wait(b_sums, 0, g.wait)))) break;
+                here = true;
                 auto add = [&](int j, unsigned w) {
                     if constexpr (MODE == kInt8) sum[j] += w;
                     else sum[j] = __float_as_uint(__uint_as_float(sum[j]) + __uint_as_float(w));
                 };
 #pragma unroll 1
                 for (unsigned from = 0; from < (unsigned)KS; ++from) {
-                    if (from == share) {
-                        unsigned acc[kAcc];
-                        read_acc(acc_at(0, u, kAcc), kAcc, acc);
-                        loaded();
+                    if (from == share) continue;
+                    const unsigned src = slot(u, from, share);
 #pragma unroll
-                        for (int j = 0; j < kAcc; ++j) add(j, acc[j]);
-                    } else {
+                    for (int h = 0; h < kAcc; h += 32) {   // eight loads in flight
+                        uint4 w[8];
 #pragma unroll
-                        for (int h = 0; h < kAcc; h += 32) {   // eight loads in flight
-                            uint4 w[8];
+                        for (int j = 0; j < 8; ++j) w[j] = ld_shared16(src + (h / 4 + j) * 512);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) w[j] = ld_shared16(slot(u, from) + (h / 4 + j) * 512);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                add(h + 4 * j, w[j].x);
-                                add(h + 4 * j + 1, w[j].y);
-                                add(h + 4 * j + 2, w[j].z);
-                                add(h + 4 * j + 3, w[j].w);
-                            }
+                        for (int j = 0; j < 8; ++j) {
+                            add(h + 4 * j, w[j].x);
+                            add(h + 4 * j + 1, w[j].y);
+                            add(h + 4 * j + 2, w[j].z);
+                            add(h + 4 * j + 3, w[j].w);
                         }
                     }
                 }
                 patch_free();
                 ok = finish(at, col, std::integral_constant<int, 32>(), sum, e, rs, cb) && ok;
             }
+            if (ok && !here) ok = __all_sync(0xFFFFFFFFu, bar_wait(b_sums, 0, g.wait));   // (nothing is sent to a CTA that has left)
         }
     }
+    // No CTA of the cluster leaves, or gives up its TMEM, while another still works on its memory.  Nothing is handed over (what a
+    // warp has sent or signalled has been waited for where it arrives), so the arrival neither releases nor waits for the stores.
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     if (warp >= 4) {
         if (!ok && lane == 0) atomicExch(g.status, 3);
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
     }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    cluster_barrier();   // no CTA of the cluster leaves, or gives up its TMEM, while another still works on its memory
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (warp == 2) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");

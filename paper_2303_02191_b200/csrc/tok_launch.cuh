@@ -54,7 +54,10 @@ struct Shape {
     int bn, KS;
     double clocks;
 };
-inline Shape choose_shape(const Product* ps, int np, bool gated, int kper, int sms) {
+template <int MODE, typename T>
+Shape choose_shape(const Product* ps, int np, int sms) {
+    constexpr bool gated = MODE == kGated;
+    constexpr int kper = MODE == kInt8 ? 128 : 64;
     const int pairs = sms / 2;
     Shape best = {256, 1, 1e300};
     for (int bn = 256; bn >= 128; bn -= 128) {
@@ -73,6 +76,7 @@ inline Shape choose_shape(const Product* ps, int np, bool gated, int kper, int s
         const double per_kb = bn == 256 ? 512.0 : 400.0;
         for (int ks = 1; ks <= kMaxKS && ks <= shares; ks *= 2) {
             if (ks > 1 && (np > 1 || kb_min < 4 * ks || tiles * ks > pairs)) continue;
+            if ((bn == 256 ? GemmShape<MODE, 256, T>::stages_of(ks) : GemmShape<MODE, 128, T>::stages_of(ks)) < 3) continue;
             const double waves = (double)((tiles * ks + pairs - 1) / pairs);
             const double c = ks == 1 ? (waves < 4 ? waves * kb * per_kb : work / pairs * per_kb) + 2000.0
                                      : (double)((kb + ks - 1) / ks) * per_kb + 6000.0 + 512.0 * bn * (ks - 1) / ks / 24.0;
@@ -102,6 +106,7 @@ int launch_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np
     }
     g.n_problems = np;
     g.KS = KS;
+    g.stages = S::stages_of(KS);
     g.a_mn = a_mn;
     g.b_mn = b_mn;
     g.status = ctx->dev_status;
