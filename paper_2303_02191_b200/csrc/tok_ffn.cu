@@ -59,7 +59,7 @@ rtoss_status check(rtoss_ctx* ctx, const rtoss_ffn* f, bool backward, const char
 
 template <typename T, int MODE, int NP>
 int run_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np, bool a_mn, bool b_mn, cudaStream_t s) {
-    const Shape c = choose_shape<MODE, T>(ps, np, ctx->sm_count > 0 ? ctx->sm_count : 148);
+    const Shape c = choose_shape<T, MODE, NP>(ctx, ps, np);
     return c.bn == 256 ? launch_gemm<T, MODE, 256, NP>(ctx, g, ps, np, a_mn, b_mn, c.KS, s) : launch_gemm<T, MODE, 128, NP>(ctx, g, ps, np, a_mn, b_mn, c.KS, s);
 }
 

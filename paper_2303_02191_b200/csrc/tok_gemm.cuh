@@ -19,7 +19,7 @@
 //     eight row tiles, so that the tiles in flight share their operands in L2.
 //   * Products with few tiles are cut along k: the pairs of a cluster of 2 KS CTAs take a share of k each, and send their sums to
 //     the pair that finishes a piece of the tile (st.async into its shared memory, counted by a barrier there; with barriers of
-//     the whole cluster on both sides the exchange took 8000 clocks, so EXCH).  The order of adding is fixed.
+//     the whole cluster on both sides the exchange took 8000 clocks, so 3000).  The order of adding is fixed.
 //   * Every wait is bounded; one that runs out leaves a code in the context's status word and the CTA goes through the normal
 //     exit (TMEM is always released).
 #ifndef RTOSS_TOK_GEMM_CUH
@@ -84,6 +84,7 @@ struct GemmShape {
     static constexpr int kUnitAcc = MODE == kPlain || MODE == kGated ? 64 : 32;   // accumulators a lane handles at a time
     static constexpr int kUnitCols = MODE == kPlain ? 64 : 32;                     // output columns of such a unit
     static constexpr int kUnits = BN / kUnitAcc;
+    static constexpr int kUnitClocks = MODE == kInt8 ? 2800 : MODE == kGateGrad ? 3700 : 1500;   // of a warp's unit in the epilogue (traced)
     static constexpr int kOutRow = kUnitCols * (int)sizeof(T);                     // bytes of a staged output row: 64 or 128
     static constexpr int kOuts = MODE == kGated || MODE == kGateGrad ? 3 : 1;
     static constexpr int kPatch = kOutRow * 32;                                    // bytes of a warp's unit of one output

@@ -173,7 +173,7 @@ int multiply(const rtoss_ctx* ctx, const rtoss_i8_product* p, cudaStream_t s) {
     g.res = p->residual.dev, g.res_ld = r_ld, g.res_after = p->residual_after_act;
     g.row_scale = p->x_scale_dev, g.col_scale = p->w_scale_dev, g.bias = p->bias_dev;
     const Product d = {(int)p->tokens, p->N, p->K, 1, {x, x}, {w, w}, {{p->y.dev, y_ld}, {}, {}}};
-    const Shape c = choose_shape<kInt8, T>(&d, 1, ctx->sm_count > 0 ? ctx->sm_count : 148);
+    const Shape c = choose_shape<T, kInt8, 1>(ctx, &d, 1);
     return c.bn == 256 ? launch_gemm<T, kInt8, 256, 1>(ctx, g, &d, 1, false, false, c.KS, s) : launch_gemm<T, kInt8, 128, 1>(ctx, g, &d, 1, false, false, c.KS, s);
 }
 

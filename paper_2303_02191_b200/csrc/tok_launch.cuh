@@ -26,60 +26,71 @@ template <> struct MapType<float> { static constexpr CUtensorMapDataType v = CU_
 template <> struct MapType<__nv_bfloat16> { static constexpr CUtensorMapDataType v = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16; };
 template <> struct MapType<__half> { static constexpr CUtensorMapDataType v = CU_TENSOR_MAP_DATA_TYPE_FLOAT16; };
 
-// How many clusters of 2 KS CTAs (one CTA an SM) the device holds at once.
-template <typename Kernel>
-int resident_clusters(Kernel kernel, int smem, int cluster, int sms) {
+// How many clusters of 2 KS CTAs (one CTA an SM) the device holds at once: a cluster's CTAs lie in one group of SMs, so fewer than
+// the SMs would make.  Asked once for each kernel and device; a CUDA error's code, negative, if it cannot be.
+template <typename T, int MODE, int BN, int NP>
+int held_clusters(const rtoss_ctx* ctx, int KS) {
+    using S = GemmShape<MODE, BN, T>;
+    auto kernel = tok_gemm_kernel<T, MODE, BN, NP>;
+    static std::atomic<int> held[3][64];   // 0: not asked yet
+    const int dev = ctx->device, sms = ctx->sm_count > 0 ? ctx->sm_count : 148, at = KS == 1 ? 0 : KS == 2 ? 1 : 2;
+    int n = dev < 64 ? held[at][dev].load(std::memory_order_acquire) : 0;
+    if (n) return n;
+    if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem)) return -(int)e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(sms / cluster * cluster));
+    cfg.gridDim = dim3((unsigned)(sms / (2 * KS) * 2 * KS));
     cfg.blockDim = dim3(kGemmThreads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
+    cfg.dynamicSmemBytes = (size_t)S::kSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)(2 * KS);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
     cfg.numAttrs = 1;
-    int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
         cudaGetLastError();
-        n = sms / cluster;
+        n = sms / (2 * KS);
     }
+    if (dev < 64) held[at][dev].store(n, std::memory_order_release);
     return n;
 }
 
-// Shape of a launch.  Clocks of a block of 128 bytes of k: 4 instructions of 128 clocks (256 columns) or, bound by what shared
-// memory moves, about 4 x 100 (128 columns).  Shares of k cost the exchange: two barriers of the cluster and reading the sums, about
-// 4000 clocks, and what a CTA sends at 24 bytes a clock (traced).
+// Shape of a launch, by the clocks that it takes (fitted to 23 products of 64 to 51200 rows, each timed in every shape): 540 for a
+// block of 128 bytes of k (256 columns; 128 columns: 480, bound by what an SM takes in), the epilogue of a unit of a warp
+// (kUnitClocks), which runs under the next tile's products, and 2000 to begin and end.  KS shares of k divide both, and cost
+// 1000 KS + 600 for the exchange (twice that in the gated block, which sends two sums a value): 331 x 1003 x 1001 in 8 bits, 16 tiles, takes 8.5 us, in two shares 7.4; 128 x 8192 x 1024
+// takes 22.3, 14.1 and 10.3 us in one, two and four.
 struct Shape {
     int bn, KS;
     double clocks;
 };
-template <int MODE, typename T>
-Shape choose_shape(const Product* ps, int np, int sms) {
+template <typename T, int MODE, int NP>
+Shape choose_shape(const rtoss_ctx* ctx, const Product* ps, int np) {
     constexpr bool gated = MODE == kGated;
     constexpr int kper = MODE == kInt8 ? 128 : 64;
-    const int pairs = sms / 2;
+    const int pairs = (ctx->sm_count > 0 ? ctx->sm_count : 148) / 2;
     Shape best = {256, 1, 1e300};
     for (int bn = 256; bn >= 128; bn -= 128) {
         const int tn = gated ? bn / 2 : bn, shares = bn / (gated ? 64 : 32);
         int64_t tiles = 0;
         int kb = 0, kb_min = 1 << 30;
         double work = 0;
+        const double per_kb = bn == 256 ? 540.0 : 480.0, finish = GemmShape<MODE, 128, T>::kUnitClocks * (GemmShape<MODE, 128, T>::kUnits / 2) * (bn / 128);
         for (int i = 0; i < np; ++i) {
             const int64_t t = (int64_t)((ps[i].M + 255) / 256) * ((ps[i].N + tn - 1) / tn);
             const int k = (ps[i].K + kper - 1) / kper * ps[i].segments;
             tiles += t;
-            work += (double)t * k;
+            work += (double)t * (k * per_kb > finish ? k * per_kb : finish);
             kb = k > kb ? k : kb;
             kb_min = k < kb_min ? k : kb_min;
         }
-        const double per_kb = bn == 256 ? 512.0 : 400.0;
         for (int ks = 1; ks <= kMaxKS && ks <= shares; ks *= 2) {
             if (ks > 1 && (np > 1 || kb_min < 4 * ks || tiles * ks > pairs)) continue;
+            if (ks > 1 && tiles > (bn == 256 ? held_clusters<T, MODE, 256, NP>(ctx, ks) : held_clusters<T, MODE, 128, NP>(ctx, ks))) continue;
             if ((bn == 256 ? GemmShape<MODE, 256, T>::stages_of(ks) : GemmShape<MODE, 128, T>::stages_of(ks)) < 3) continue;
-            const double waves = (double)((tiles * ks + pairs - 1) / pairs);
-            const double c = ks == 1 ? (waves < 4 ? waves * kb * per_kb : work / pairs * per_kb) + 2000.0
-                                     : (double)((kb + ks - 1) / ks) * per_kb + 6000.0 + 512.0 * bn * (ks - 1) / ks / 24.0;
+            const double waves = (double)((tiles * ks + pairs - 1) / pairs), tile = kb * per_kb > finish ? kb * per_kb : finish;
+            const double c = ks == 1 ? (waves < 2 ? kb * per_kb : waves < 4 ? waves * tile : work / pairs) + finish
+                                     : (double)((kb + ks - 1) / ks) * per_kb + finish / ks + (1000.0 * ks + 600.0) * (gated ? 2.0 : 1.0);
             if (c < best.clocks) best = {bn, ks, c};
         }
     }
@@ -93,17 +104,10 @@ int launch_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np
     constexpr bool i8 = MODE == kInt8;
     const CUtensorMapDataType in_type = i8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : MapType<T>::v;
     const int in_size = i8 ? 1 : 2, kper = 128 / in_size;
-    static std::atomic<int> resident[64];   // pairs the device holds at once; 0: not asked yet
-    const int sms = ctx->sm_count > 0 ? ctx->sm_count : 148;
-    const int dev = ctx->device;
     // (the driver encodes for the thread's current context, and a thread that has made no runtime call yet has none)
-    if (const cudaError_t e = cudaSetDevice(dev)) return (int)e;
-    int held = dev < 64 ? resident[dev].load(std::memory_order_acquire) : 0;
-    if (!held) {
-        if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem)) return (int)e;
-        held = resident_clusters(kernel, S::kSmem, 2, sms);
-        if (dev < 64) resident[dev].store(held, std::memory_order_release);
-    }
+    if (const cudaError_t e = cudaSetDevice(ctx->device)) return (int)e;
+    const int held = held_clusters<T, MODE, BN, NP>(ctx, KS);
+    if (held < 0) return -held;
     g.n_problems = np;
     g.KS = KS;
     g.stages = S::stages_of(KS);
@@ -154,7 +158,7 @@ int launch_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np
     if (!ok) return (int)cudaErrorInvalidValue;
     if (tiles > 0x3FFFFFFF) return (int)cudaErrorInvalidConfiguration;
     g.tiles = (int)tiles;
-    const int64_t clusters = KS > 1 ? tiles : tiles < held ? tiles : held;
+    const int64_t clusters = KS > 1 ? tiles : tiles < held ? tiles : held;   // (KS > 1: a tile each, choose_shape sees to it that all are held)
     return (int)rtoss_dev::launch_pdl(kernel, dim3((unsigned)(clusters * 2 * KS)), dim3(kGemmThreads), (size_t)S::kSmem, stream, 2 * KS, g);
 }
 
