@@ -13,7 +13,7 @@
 //     into shared memory in rows of 128 bytes with the 128-byte swizzle, and the instruction descriptor says which it is:
 //     nothing is transposed in memory.
 //   * Warp roles: warp 0 issues TMA copies, warp 1 of the leader issues tcgen05.mma, warp 2 owns the TMEM allocation, eight
-//     epilogue warps read the accumulators (two stages: the epilogue of a tile runs under the products of the next), round
+//     or sixteen epilogue warps read the accumulators (two stages: the epilogue of a tile runs under the products of the next), round
 //     into shared memory and leave the rest to TMA stores, which also cut off what lies outside the matrix.
 //   * CTA pairs are persistent and walk the tiles of up to three products (the weight gradients of the block) in groups of
 //     eight row tiles, so that the tiles in flight share their operands in L2.
@@ -42,8 +42,6 @@ enum GemmMode {
     kInt8 = 3       // 8-bit operands: scales, bias, activation, residual
 };
 
-constexpr int kGemmThreads = 384;
-constexpr int kEpiWarps = 8;
 constexpr int kMaxKS = 4;   // shares of k: clusters of at most 8 CTAs
 
 struct GemmProblem {
@@ -78,6 +76,10 @@ struct GemmArgs {
 // ---- shapes of a kernel -------------------------------------------------------------------------------------------
 template <int MODE, int BN, typename T>
 struct GemmShape {
+    // Epilogue warps: sixteen for the narrow tiles of the 8-bit product, whose k is often short, so that the activation of one warp runs
+    // while others wait for copies (51200 x 128 x 128 with SiLU: 13.7 us with eight, 12.0 with sixteen).
+    static constexpr int kEpiWarps = MODE == kInt8 && BN == 128 ? 16 : 8, kSides = kEpiWarps / 4;
+    static constexpr int kThreads = 128 + 32 * kEpiWarps;
     static constexpr int kABytes = 128 * 128;
     static constexpr int kBBytes = BN / 2 * 128;
     static constexpr int kStageBytes = kABytes + kBBytes;
@@ -89,13 +91,15 @@ struct GemmShape {
     static constexpr int kOuts = MODE == kGated || MODE == kGateGrad ? 3 : 1;
     static constexpr int kPatch = kOutRow * 32;                                    // bytes of a warp's unit of one output
     static constexpr int kSet = kPatch * kOuts;
-    // kGateGrad: two sets, whose patches take the saved projections before their gradients; kInt8: column scales and biases
-    static constexpr int kStagingBytes = MODE == kGateGrad ? 2 * kSet : kSet + (MODE == kInt8 ? 1024 : 0);
+    // kGateGrad: two sets, whose patches take the saved projections before their gradients; kInt8: column scales and biases behind
+    // all patches
+    static constexpr int kWarpBytes = MODE == kGateGrad ? 2 * kSet : kSet;
+    static constexpr int kStagingBytes = kEpiWarps * (kWarpBytes + (MODE == kInt8 ? 256 : 0));
     // columns of accumulators that the CTAs of a split tile deal out, and what they make of the output
     static constexpr int kShareAcc = MODE == kGated ? 64 : 32, kShares = BN / kShareAcc;                     // of a warp
-    static constexpr int kRoom = 226 * 1024 - kEpiWarps * kStagingBytes;
+    static constexpr int kRoom = 227 * 1024 - 1536 - kStagingBytes;
     static constexpr int kStages = kRoom / kStageBytes < 8 ? kRoom / kStageBytes : 8;
-    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStagingBytes + 1024 + 512;
+    static constexpr int kSmem = kStages * kStageBytes + kStagingBytes + 1024 + 512;
     static constexpr int kTileN = MODE == kGated ? BN / 2 : BN;                    // output columns of a tile
     static constexpr int kTmemCols = 2 * BN;
     // Stages that KS pairs leave of the ring beside what each receives: the sums of KS - 1 others for its BN / KS columns.
@@ -234,9 +238,6 @@ template <> __device__ __forceinline__ unsigned pack_pair<__half>(float lo, floa
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const unsigned*>(&v);
 }
-template <typename T> __device__ __forceinline__ float2 unpack_pair(unsigned v);
-template <> __device__ __forceinline__ float2 unpack_pair<__nv_bfloat16>(unsigned v) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&v)); }
-template <> __device__ __forceinline__ float2 unpack_pair<__half>(unsigned v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
 
 // COLS values of a lane's row into its place in the warp's staging patch, in 16-byte pieces where the TMA store with the
 // 128-byte (64-byte) swizzle looks for them; the lanes of a piece hit different banks.
@@ -313,18 +314,18 @@ __device__ __forceinline__ float value_of(const uint4* e, int j) {
     const unsigned* w = reinterpret_cast<const unsigned*>(e);
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
     else {
-        const float2 p = unpack_pair<T>(w[j >> 1]);
+        const float2 p = widen2<T>(w[j >> 1]);
         return j & 1 ? p.y : p.x;
     }
 }
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------
 template <typename T, int MODE, int BN, int NP>
-__global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_constant__ GemmArgs<NP> g) {
+__global__ void __launch_bounds__((GemmShape<MODE, BN, T>::kThreads), 1) tok_gemm_kernel(const __grid_constant__ GemmArgs<NP> g) {
     using S = GemmShape<MODE, BN, T>;
     extern __shared__ unsigned char smem_raw[];
     const unsigned raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    const unsigned s_stage = base, s_out = base + S::kStages * S::kStageBytes, s_bar = s_out + kEpiWarps * S::kStagingBytes;
+    const unsigned s_stage = base, s_out = base + S::kStages * S::kStageBytes, s_bar = s_out + S::kStagingBytes;
     const unsigned b_full = s_bar, b_empty = s_bar + 64, b_acc_full = s_bar + 128, b_acc_empty = s_bar + 144, s_tmem = s_bar + 160, b_edge = s_bar + 176, b_sums = s_bar + 304;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const unsigned rank = cta_rank(), half = rank & 1u, lead_rank = rank & ~1u, share = rank >> 1;
@@ -343,10 +344,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(b_acc_full + 8 * i, 1);
-            bar_init(b_acc_empty + 8 * i, 2 * kEpiWarps);
+            bar_init(b_acc_empty + 8 * i, 2 * S::kEpiWarps);
         }
         if (MODE == kGateGrad)
-            for (int i = 0; i < 2 * kEpiWarps; ++i) bar_init(b_edge + 8 * i, 1);
+            for (int i = 0; i < 2 * S::kEpiWarps; ++i) bar_init(b_edge + 8 * i, 1);
         if (KS > 1) {
             bar_init(b_sums, 1);
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b_sums), "r"(128 * (BN / KS) * (KS - 1) * 4) : "memory");
@@ -466,8 +467,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
     __syncwarp();
 
     // ---- epilogue ---------------------------------------------------------------------------------------------------
-    const int quad = warp & 3, side = (warp - 4) >> 2;   // 32 accumulator rows; every other unit of columns
-    const unsigned staging = s_out + (unsigned)((warp - 4) * S::kStagingBytes);
+    const int quad = warp & 3, side = (warp - 4) >> 2;   // 32 accumulator rows; every kSides-th unit of columns
+    const unsigned staging = s_out + (unsigned)((warp - 4) * S::kWarpBytes);
     auto read_acc = [&](unsigned at, int cols, unsigned* acc) {   // (not complete before tcgen05.wait::ld)
         tmem_ld32(at, acc);
         if (cols == 64) tmem_ld32(at + (MODE == kGated ? BN / 2 : 32), acc + 32);
@@ -552,7 +553,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             });
         } else {
             // the unit's column scales and biases: a lane fetches one of each, all lanes read all
-            const unsigned cols_at = patch + S::kPatch;
+            const unsigned cols_at = s_out + (unsigned)(S::kEpiWarps * S::kWarpBytes + (warp - 4) * 256);
             __syncwarp();
             asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(cols_at + 8u * (unsigned)lane), "f"(cb.x), "f"(cb.y) : "memory");
             __syncwarp();
@@ -607,28 +608,31 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
         for (int t = cluster; t < g.tiles && ok; t += clusters) {
             const Tile at = tile_of(t);
             const int col0 = at.nt * S::kTileN;
-            uint4 e[8], e_next[8];
+            constexpr bool kAhead = MODE == kInt8 && S::kUnits > S::kSides;   // a warp has several units: the next one's operands come ahead
+            uint4 e[8], e_next[kAhead ? 8 : 1];
             residual_of(at, col0 + side * S::kUnitCols, e);
             const float rs = row_scale_of(at);
             float2 cb = column_of(at, col0 + side * S::kUnitCols), cb_next = cb;
             if (!(ok = __all_sync(0xFFFFFFFFu, bar_wait(b_acc_full + 8 * as, aph, g.wait)))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-            for (int u = side; u < S::kUnits; u += 2) {
+            for (int u = side; u < S::kUnits; u += S::kSides) {
                 unsigned acc[S::kUnitAcc];
                 read_acc(acc_at(as, u, S::kUnitAcc), S::kUnitAcc, acc);
-                const int next = col0 + (u + 2) * S::kUnitCols;
-                if (u + 2 < S::kUnits) {
+                const int next = col0 + (u + S::kSides) * S::kUnitCols;
+                if (u + S::kSides < S::kUnits) {
                     ask(at, next);
-                    residual_of(at, next, e_next);
-                    cb_next = column_of(at, next);
+                    if constexpr (kAhead) {
+                        residual_of(at, next, e_next);
+                        cb_next = column_of(at, next);
+                    }
                 } else if (MODE == kGateGrad && t + clusters < g.tiles) {
                     const Tile then = tile_of(t + clusters);
                     ask(then, then.nt * S::kTileN + side * S::kUnitCols);
                 }
                 patch_free();
                 loaded();
-                if (u + 2 >= S::kUnits) {
+                if (u + S::kSides >= S::kUnits) {
                     // All sums of this tile are in registers: the pair may overwrite them.  Nothing else is handed over, and a release
                     // would wait for the stores on their way, 3000 clocks.
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -637,8 +641,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
                         asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(b_acc_empty + 8 * as, lead_rank)) : "memory");
                 }
                 ok = finish(at, col0 + u * S::kUnitCols, std::integral_constant<int, S::kUnitCols>(), acc, e, rs, cb) && ok;
-                cb = cb_next;
-                if constexpr (MODE == kInt8) {
+                if constexpr (kAhead) {
+                    cb = cb_next;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) e[j] = e_next[j];
                 }
@@ -662,7 +666,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (ok) {
 #pragma unroll 1
-            for (int v = side; v < S::kShares; v += 2) {
+            for (int v = side; v < S::kShares; v += S::kSides) {
                 const int u = (v + (int)share * per) % S::kShares;   // (each pair begins with a piece of its own, then they go round)
                 const unsigned owner = (unsigned)(u / per);
                 if (owner == share) continue;
@@ -675,8 +679,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) tok_gemm_kernel(const __grid_
             }
             bool here = false;
 #pragma unroll 1
-            for (int u = (int)share * per + (per > 1 ? side : 0); u < ((int)share + 1) * per && ok; u += per > 1 ? 2 : 1) {
-                if (per == 1 && side != 0) break;
+            for (int u = (int)share * per + side; u < ((int)share + 1) * per && ok; u += S::kSides) {
                 const int col = at.nt * S::kTileN + u * 32;
                 uint4 e[8];
                 ask(at, col);

@@ -11,8 +11,7 @@ constexpr const char* kMul = "matmul i8";
 
 // ---- rows to 8 bits -------------------------------------------------------------------------------------------------
 // bound: bytes (a row is read once and one byte a value written), if the arithmetic stays near six instructions a value: the
-// maximum is taken over the bits as they lie in memory (two 16-bit magnitudes at a time), and one fused multiply-add against
-// 1.5 * 2^23 rounds x / s and leaves the code in its low bits.  G threads take a row and hold up to 32 values each between the
+// maximum is taken over the bits as they lie in memory (two 16-bit magnitudes at a time), and nothing divides but the scales.  G threads take a row and hold up to 32 values each between the
 // maximum and the rounding; longer rows are read again, from the caches.
 constexpr int kHold = 4;   // pieces of eight values a thread holds
 
@@ -36,27 +35,46 @@ __device__ __forceinline__ void fetch8(const T* row, int i, int cols, Piece<T>& 
 template <typename T>
 __device__ __forceinline__ unsigned most_of(unsigned top, const Piece<T>& v) {
     const unsigned* w = reinterpret_cast<const unsigned*>(&v);
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) * 2; ++j)
-        top = sizeof(T) == 4 ? max(top, w[j] & 0x7FFFFFFFu) : __vmaxu2(top, w[j] & 0x7FFF7FFFu);
+        for (int j = 0; j < 8; ++j) top = max(top, w[j] & 0x7FFFFFFFu);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) top = __vimax3_u16x2(top, w[j] & 0x7FFF7FFFu, w[j + 1] & 0x7FFF7FFFu);
+    }
     return top;
 }
 
 // The code of x: the quotient x / s in fp32, rounded half to even.
 __device__ __forceinline__ int exact_code(float x, float s) { return (int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f); }
 
-// Eight codes.  x * (1 / s) is within 127 * 2^-23 < 1.6e-5 of the rounded quotient, so its nearest integer is the quotient's
-// unless it lies that close to half way; then (and for scales whose reciprocal would overflow) the division decides.
+// Eight codes.  Adding 1.5 * 2^23 rounds the quotient half to even and leaves the code in the sum's low bits.
+// 16-bit values: the quotient is corrected once by its remainder (Markstein, 1990), in four instructions for two values; for
+// every pair of 8- or 11-bit mantissas it rounds to the code of the fp32 quotient.  Half the row's maximum, which is half way
+// between two codes, is common among such values: with a division wherever a plain product with 1 / s came near half way,
+// two warps in five divided.
+// fp32: the product is within 127 * 2^-23 < 1.6e-5 of the rounded quotient, so its nearest integer is the quotient's unless it
+// lies that close to half way; then the division decides.
+// (divide: scales whose reciprocal would overflow, or whose remainders would be subnormal)
 template <typename T>
 __device__ __forceinline__ uint2 codes_of(const Piece<T>& v, float s, float inv, bool divide) {
-    constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: the sum's last bit is 1
+    constexpr float kMagic = 12582912.f;
     unsigned t[8];
     float far = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float x = rtoss_dev::to_f32<T>(v.e[j]), m = fmaf(x, inv, kMagic);
-        t[j] = __float_as_uint(m);
-        far = fmaxf(far, fabsf(fmaf(x, inv, kMagic - m)));
+    for (int j = 0; j < 4; ++j) {
+        const float2 x = pair_of<T>(v, j);
+        float2 m;
+        if constexpr (sizeof(T) == 2) {
+            const float2 q = mul2(x, both(inv));
+            m = add2(fma2(fma2(q, both(-s), x), both(inv), q), both(kMagic));
+        } else {
+            m = fma2(x, both(inv), both(kMagic));
+            const float2 d = fma2(x, both(inv), fma2(m, both(-1.f), both(kMagic)));
+            far = fmaxf(far, fmaxf(fabsf(d.x), fabsf(d.y)));
+        }
+        t[2 * j] = __float_as_uint(m.x);
+        t[2 * j + 1] = __float_as_uint(m.y);
     }
     if (divide || far > 0.5f - 2e-5f) {
 #pragma unroll

@@ -39,7 +39,7 @@ int held_clusters(const rtoss_ctx* ctx, int KS) {
     if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem)) return -(int)e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(sms / (2 * KS) * 2 * KS));
-    cfg.blockDim = dim3(kGemmThreads);
+    cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = (size_t)S::kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -159,7 +159,7 @@ int launch_gemm(const rtoss_ctx* ctx, GemmArgs<NP>& g, const Product* ps, int np
     if (tiles > 0x3FFFFFFF) return (int)cudaErrorInvalidConfiguration;
     g.tiles = (int)tiles;
     const int64_t clusters = KS > 1 ? tiles : tiles < held ? tiles : held;   // (KS > 1: a tile each, choose_shape sees to it that all are held)
-    return (int)rtoss_dev::launch_pdl(kernel, dim3((unsigned)(clusters * 2 * KS)), dim3(kGemmThreads), (size_t)S::kSmem, stream, 2 * KS, g);
+    return (int)rtoss_dev::launch_pdl(kernel, dim3((unsigned)(clusters * 2 * KS)), dim3(S::kThreads), (size_t)S::kSmem, stream, 2 * KS, g);
 }
 
 }  // namespace rtoss_tok

@@ -8,6 +8,37 @@
 
 namespace rtoss_tok {
 
+// Pairs of values: one instruction for both.
+__device__ __forceinline__ unsigned long long& bits2(float2& v) { return reinterpret_cast<unsigned long long&>(v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)));
+    return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// Two neighbouring 16-bit values as they lie in a word.  (bf16: by shift and mask.  The conversion of a single value goes through the
+// special-function pipe, which then bounds an elementwise kernel.)
+template <typename T> __device__ __forceinline__ float2 widen2(unsigned w);
+template <> __device__ __forceinline__ float2 widen2<__nv_bfloat16>(unsigned w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+template <> __device__ __forceinline__ float2 widen2<__half>(unsigned w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// Pair j of eight values.
+template <typename T, typename Eight>
+__device__ __forceinline__ float2 pair_of(const Eight& v, int j) {
+    if constexpr (sizeof(T) == 4) return make_float2(v.e[2 * j], v.e[2 * j + 1]);
+    else return widen2<T>(reinterpret_cast<const unsigned*>(&v)[j]);
+}
+
 // f(std::integral_constant<int, ACT>): the activation is decided once for a run of elements
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F&& f) {

@@ -43,25 +43,6 @@ struct NormArgs {
     void* dgate;
 };
 
-// ---- pairs of values: one instruction for both -------------------------------------------------------------------------
-__device__ __forceinline__ unsigned long long& bits2(float2& v) { return reinterpret_cast<unsigned long long&>(v); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(bits2(d)) : "l"(bits2(a)), "l"(bits2(b)));
-    return d;
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-
 // ---- eight values -----------------------------------------------------------------------------------------------------
 // As they lie in memory: a row's loads stay in flight until its values are widened.
 template <typename T>
@@ -88,7 +69,7 @@ __device__ __forceinline__ void zero8(Raw<T>& r) {
 template <typename T>
 __device__ __forceinline__ void widen8(const Raw<T>& r, float2 (&v)[4]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = make_float2(to_f32<T>(r.e[2 * j]), to_f32<T>(r.e[2 * j + 1]));
+    for (int j = 0; j < 4; ++j) v[j] = pair_of<T>(r, j);
 }
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const void* base, long long ld, int row, int i, int D, float2 (&v)[4]) {

@@ -186,3 +186,22 @@ def test_pruned_pointwise_layer_in_eight_bits():
     rms = ref.square().mean().sqrt()
     within(y, want.reshape(-1, Cout).double(), tol + 2e-4 * torch.maximum(ref.abs(), rms), "y")   # (the convolution's own bound: 1e-4)
     packed.close()
+
+
+@pytest.mark.parametrize("dt,bits", [("bf16", 7), ("f16", 10)])
+def test_codes_of_every_mantissa_against_every_maximum(dt, bits):
+    """A code depends on the mantissas of a value and of its row's maximum and on how far their exponents lie apart: all of them, below
+    a tenth of a step left out, for maxima of several exponents.  The codes are those of the fp32 quotient, half to even."""
+    n = 1 << bits
+    m = torch.arange(n, 2 * n, dtype=torch.float64) / n
+    x = torch.cat([m * 2.0 ** -e for e in range(0, 11)]).to(DT[dt])
+    for scale in (1.0, 2.0 ** -9, 1024.0) + ((2.0 ** 100, 2.0 ** -95, 2.0 ** -110) if dt == "bf16" else ()):
+        rows = x.double()[None, :].repeat(n, 1) * scale
+        rows = torch.where(rows <= (m * scale)[:, None], rows, 0.0)
+        rows[:, 1::2] *= -1
+        rows[:, 0] = m * scale
+        xd = rows.to(DT[dt]).cuda()
+        q, s = torch.empty(n, x.numel(), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        ctx().rtoss_quantize_rows(xd, q, s)
+        want_q, want_s = codes_of(xd)
+        assert torch.equal(s.cpu(), want_s) and torch.equal(q.cpu(), want_q), (dt, scale)
