@@ -48,6 +48,10 @@ SYMBOLS = [
 _I8_PRODUCT = struct.Struct("@q2i" + "Qq" * 4 + "3Q3i4x")
 _FFN = struct.Struct("@q4i" + "Qq" * 15)
 _BLOCK_NORM = struct.Struct("@q4i2fq2Q" + "Qq" * 10 + "3Qq")
+# (the forward calls': the fields of the backward pass are zeros)
+_FFN_FORWARD = struct.Struct("@q4i" + "Qq" * 8 + "112x")
+_BLOCK_NORM_FORWARD = struct.Struct("@q4i2fq2Q" + "Qq" * 5 + "112x")
+assert _FFN_FORWARD.size == _FFN.size and _BLOCK_NORM_FORWARD.size == _BLOCK_NORM.size
 
 
 class RtossError(RuntimeError):
@@ -617,11 +621,11 @@ class Context:
         tokens, D = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
         F, t, d = w_gate.size(0) if w_gate.dim() == 2 else _bad("w_gate", "need a matrix"), x.dtype, self.device
         row, mid, win, wout = (tokens, D), (tokens, F), (F, D), (D, F)
-        st = lib.rtoss_gated_ffn_forward(self.h, _FFN.pack(
+        st = lib.rtoss_gated_ffn_forward(self.h, _FFN_FORWARD.pack(
             tokens, D, F, _torch_dtype_code(x), act, *_matrix(x, row, t, d, "x"), *_matrix(w_gate, win, t, d, "w_gate"),
             *_matrix(w_up, win, t, d, "w_up"), *_matrix(w_down, wout, t, d, "w_down"), *_matrix(h, mid, t, d, "h"),
-            *_matrix(gate, mid, t, d, "gate"), *_matrix(up, mid, t, d, "up"), *_matrix(y, row, t, d, "y"),
-            0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
+            *_matrix(gate, mid, t, d, "gate"), *_matrix(up, mid, t, d, "up"), *_matrix(y, row, t, d, "y")),
+            _stream_on(d))
         if st:
             self._check(st)
         return h if y is None else y
@@ -653,11 +657,11 @@ class Context:
         row = tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
         t, d, each = y.dtype, self.device, (D,)
         share = tokens_per_gate or max(tokens, 1)
-        st = lib.rtoss_block_norm_forward(self.h, _BLOCK_NORM.pack(
+        st = lib.rtoss_block_norm_forward(self.h, _BLOCK_NORM_FORWARD.pack(
             tokens, D, _torch_dtype_code(y), post, pre, residual_scale, eps, share, _vector(post_weight, each, _F32, d, "post_weight"),
             _vector(pre_weight, each, _F32, d, "pre_weight"), *_matrix(r, row, t, d, "r"), *_matrix(y, row, t, d, "y"),
             *_matrix(gate, (max(tokens // share, 1), D), t, d, "gate"), *_matrix(z, row, t, d, "z"),
-            *_matrix(n, row, t, d, "n"), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), _stream_on(d))
+            *_matrix(n, row, t, d, "n")), _stream_on(d))
         if st:
             self._check(st)
         return z, n
