@@ -240,3 +240,15 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for m, ref in zip((a, b), refs):
         check(m, ref, BOTH)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("T,D,F", [(200, 1024, 2816), (100, 4096, 512), (300, 2048, 264), (40, 520, 4100)])
+def test_products_cut_along_k(T, D, F, dt):
+    """Few tiles and a long k: shares of k, exchanged between the CTAs of a cluster."""
+    m = setup(T, D, F, dt, pad=T % 3)
+    ref = reference(m, "silu", dt)
+    forward(m, "silu")
+    check(m, ref, FWD)
+    backward(m, "silu")
+    check(m, ref, BWD + ("h_again",))

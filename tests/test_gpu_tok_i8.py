@@ -205,3 +205,10 @@ def test_codes_of_every_mantissa_against_every_maximum(dt, bits):
         ctx().rtoss_quantize_rows(xd, q, s)
         want_q, want_s = codes_of(xd)
         assert torch.equal(s.cpu(), want_s) and torch.equal(q.cpu(), want_q), (dt, scale)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,K,N", [(128, 8192, 1000), (331, 1003, 1001), (200, 4096, 4096), (64, 2048, 520), (1000, 1030, 1024)])
+def test_products_cut_along_k(T, K, N, dt):
+    """Few tiles and a long k: shares of k, exchanged between the CTAs of a cluster."""
+    product(T, K, N, dt, act="silu", bias=True, res="before" if T % 2 else "after", pad=1)

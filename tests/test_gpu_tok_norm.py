@@ -257,3 +257,30 @@ def test_same_bits_every_time_and_in_graphs_with_their_own_workspaces():
     for q in (m, m2):
         for k in names:
             assert torch.equal(get(q, k), first[k]), k
+
+
+# D of every way that rows are dealt out: units of 8, 16 and 32 threads, blocks that are not full, two pieces a thread; rows enough
+# for several to a unit, with gates that begin and end inside blocks
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,D,gates", [(9000, 64, 18), (4100, 72, 0), (5000, 128, 10), (9000, 200, 9), (4900, 264, 7), (2000, 648, 0), (1800, 1280, 6), (800, 2056, 2),
+                                       (900, 2560, 30), (333, 4104, 0), (400, 5000, 5)])
+def test_rows_of_every_length(T, D, gates, dt):
+    kinds = ("rms", "layer", "none")
+    post, pre = kinds[(T // 100 + D) % 2], kinds[D // 8 % 3]
+    m = setup(T, D, dt, gates)
+    ref = reference(m, T, D, post, pre, gates, dt)
+    forward(m, T, post, pre, gates)
+    backward(m, T, post, pre, gates)
+    check(m, ref, ALL)
+    assert ctx().rtoss_device_status() == 0
+
+
+def test_weights_that_start_anywhere():
+    T, D = 40, 512
+    m = setup(T, D, "bf16", 0)
+    for k in ("wpost", "wpre"):
+        m[k] = torch.cat([torch.zeros(1, device="cuda"), m[k]])[1:]
+    ref = reference(m, T, D, "rms", "layer", 0, "bf16")
+    forward(m, T, "rms", "layer", 0)
+    backward(m, T, "rms", "layer", 0)
+    check(m, ref, ALL)
