@@ -604,7 +604,8 @@ rtoss_status rtoss_gated_ffn_backward(rtoss_ctx* ctx, const rtoss_ffn* ffn, void
  * same with t's mean subtracted first; RTOSS_NORM_NONE: v = y resp. no n.  Weights are fp32 [D] (NULL: ones).  The gate
  * (dev NULL: none) has one row of D values in the data type for every tokens_per_gate consecutive tokens (tokens: one
  * learned gate for all; fewer: one per sample); it must divide the tokens.  n is taken from z before z is rounded.
- * fp32, bf16 or fp16 data, any strides and alignment (rows on 16-byte boundaries with D a multiple of 8 are faster);
+ * fp32, bf16 or fp16 data, any strides and alignment (rows and weights on 16-byte boundaries with D a multiple of 8 are
+ * faster);
  * fp32 arithmetic, rounded once.  z may be r or y itself, and so may n (not the same one as z).
  * Backward, from r, y and the gradients dz and dn of z and n (each may be NULL = zero): dr, dy and, where not NULL,
  * dpost_weight, dpre_weight (fp32 [D]) and dgate (like gate, summed over the tokens that share it).  v and z are formed

@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) tok_few_kernel(const FewArgs a
     // pieces of 16 bytes: this block takes [first, last), a warp kUnroll groups of four at a time
     const int pieces = (a.K + kPer - 1) / kPer, first = (int)rank * a.share, last = min(pieces, first + a.share);
     // (loads without conditions, all in flight at once, but for the last round and rows whose end cuts a piece: with conditions
-    // the block of one token, 2048 -> 5632, took 27 us, without them 15)
+    // the block of one token, 2048 -> 5632, took 20.9 us, without them 15.0, 4.6 TB/s)
     const int all = min(last, a.K / kPer);
     for (int p0 = first + warp * 4 * kUnroll; p0 < last; p0 += kFewWarps * 4 * kUnroll) {
         uint4 wa[kUnroll], wb[kUnroll], xb[kUnroll][NT];

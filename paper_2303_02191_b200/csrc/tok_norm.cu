@@ -12,6 +12,9 @@
 // tokens (the gradients of weights and gates) end as one row per block in the workspace and are added in the blocks' order by
 // a second launch: no atomics, the same bits every time.  All arithmetic is fp32; squares are summed after the mean is
 // subtracted, not as a difference of moments.
+// Measured (bf16, cold): 16384 x 2048 forward 45.4 us, 5.9 TB/s; 8192 x 2048 forward 29.9, backward 55 (3.7 TB/s) and the sums over
+// tokens 8.5.  The backward pass is bound by its chain: a row's four sums over the block follow one another, with three rows
+// at a time on an SM.
 #include <atomic>
 
 #include "tok_internal.h"
@@ -166,7 +169,7 @@ constexpr int blocks_of() { return threads_of<G, P, BACKWARD>() / block_of<G>();
 
 // Rows on their way to a unit, A operands of each.  RING: a block's rows come by bulk copies through a ring of stages in shared
 // memory, up to `stages` rows ahead of the one at work (with one row ahead in registers an SM had 32 KB in flight, too little
-// for 6.5 TB/s: 16384 x 2048 forward took 68 us, with the ring 51).  Otherwise (rows off 16-byte boundaries, and units of up to
+// for 6.5 TB/s: 16384 x 2048 forward took 68 us, with the ring 46).  Otherwise (rows off 16-byte boundaries, and units of up to
 // a warp, whose rows are too short for a copy each) the next row waits in registers.
 template <typename T, bool VEC, int G, int P, int A>
 struct RowFeed {
