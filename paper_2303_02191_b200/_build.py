@@ -64,6 +64,7 @@ def _fingerprint():
 
 
 def build(verbose=False, force=False):
+    build_calls()
     stamp = LIB + ".stamp"
     fp = _fingerprint()
     if not force and not verbose and os.path.exists(LIB) and os.path.exists(stamp) and open(stamp).read().strip() == fp:
@@ -81,6 +82,39 @@ def build(verbose=False, force=False):
         subprocess.check_call(cmd)
     open(stamp, "w").write(fp)
     return LIB
+
+
+CALLS = os.path.join(PKG, "_tok_calls.so")
+CALLS_SRC = os.path.join(PKG, "native", "tok_calls.cpp")
+
+
+def calls_fingerprint():
+    """What _tok_calls.so was built from and for: its source, the boundary, and the interpreter and torch whose objects it reads."""
+    import hashlib
+    import torch
+    h = hashlib.sha256(("%s %s" % (sys.version, torch.__version__)).encode())
+    for f in (CALLS_SRC, os.path.join(INC, "rtoss.h")):
+        h.update(open(f, "rb").read())
+    return h.hexdigest()
+
+
+def build_calls():
+    """Build the extension module behind the operators over tokens (host code); without torch there is nothing for it to read."""
+    import sysconfig
+    try:
+        import torch
+    except ImportError:
+        return None
+    stamp, fp = CALLS + ".stamp", calls_fingerprint()
+    if os.path.exists(CALLS) and os.path.exists(stamp) and open(stamp).read().strip() == fp:
+        return CALLS
+    from torch.utils import cpp_extension
+    inc = [INC, sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")] + cpp_extension.include_paths()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    cmd += [f for d in inc for f in ("-isystem", d)] + [CALLS_SRC, "-o", CALLS, "-L", os.path.join(os.path.dirname(torch.__file__), "lib")]
+    subprocess.check_call(cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+    open(stamp, "w").write(fp)
+    return CALLS
 
 
 if __name__ == "__main__":

@@ -408,14 +408,26 @@ def _vector(t, shape, dtype, device, what):
     return t.data_ptr()
 
 
-_F32 = _I8 = None
+_F32 = _I8 = _calls = None
 
 
 def _types():
-    """torch's types, looked up once (an import statement in every call costs a tenth of a small call)."""
-    global _F32, _I8
+    """torch's types, looked up once, and the extension module that looks at operands without Python (native/tok_calls.cpp).  Where
+    that was not built for this interpreter and torch, the checks below do, at 0.5 us a tensor."""
+    global _F32, _I8, _calls
     import torch
-    _F32, _I8 = torch.float32, torch.int8
+    from . import _build
+    if os.path.exists(_build.CALLS) and os.path.exists(_build.CALLS + ".stamp") and \
+            open(_build.CALLS + ".stamp").read().strip() == _build.calls_fingerprint():
+        import importlib.util
+        spec = importlib.util.spec_from_file_location("_tok_calls", _build.CALLS)
+        calls = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(calls)
+        calls.entries(*[ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+            "rtoss_quantize_rows", "rtoss_matmul_i8", "rtoss_gated_ffn_forward", "rtoss_gated_ffn_backward", "rtoss_block_norm_forward",
+            "rtoss_block_norm_backward")])
+        _calls = calls
+    _I8, _F32 = torch.int8, torch.float32
 
 
 class Context:
@@ -427,12 +439,14 @@ class Context:
         if st != OK:
             raise RtossError(st, "rtoss_create: " + status_string(st) + " (a CUDA device is required)")
         self.h = h
+        self._h = h.value      # (as a number, for _tok_calls)
         self.device = device
 
     def close(self):
         if self.h:
             lib.rtoss_destroy(self.h)
             self.h = None
+            self._h = 0
 
     def __del__(self):
         try:
@@ -590,6 +604,12 @@ class Context:
         """x [rows, cols] fp32 / bf16 / fp16 -> int8 codes q [rows, cols] and fp32 scale [rows]."""
         if _F32 is None:
             _types()
+        if _calls is not None:
+            st = _calls.quantize_rows(self._h, self.device, x, q, scale)
+            if st == 0:
+                return q, scale
+            if st > 0:
+                self._check(st)
         shape = rows, cols = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
         xp, xs = _matrix(x, shape, x.dtype, self.device, "x")
         qp, qs = _matrix(q, shape, _I8, self.device, "q")
@@ -603,6 +623,12 @@ class Context:
         """y [tokens, N] = act(x_scale * w_scale * (x [tokens, K] @ w [N, K]^T) + bias + residual)."""
         if _F32 is None:
             _types()
+        if _calls is not None:
+            st = _calls.matmul_i8(self._h, self.device, x, x_scale, w, w_scale, y, act, bias, residual, 1 if residual_after_act else 0)
+            if st == 0:
+                return y
+            if st > 0:
+                self._check(st)
         tokens, K = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
         N, d, t = w.size(0) if w.dim() == 2 else _bad("w", "need a matrix"), self.device, y.dtype
         out, each = (tokens, N), (N,)
@@ -618,6 +644,14 @@ class Context:
     def rtoss_gated_ffn_forward(self, x, w_gate, w_up, w_down, h, y, gate=None, up=None, act=ACT_SILU):
         """h [tokens, F] = act(x w_gate^T) * (x w_up^T), y [tokens, D] = h w_down^T; gate, up: kept for the backward pass.
         w_down and y may be None together.  Returns y, or h."""
+        if _F32 is None:
+            _types()
+        if _calls is not None:
+            st = _calls.gated_ffn_forward(self._h, self.device, x, w_gate, w_up, w_down, h, y, gate, up, act)
+            if st == 0:
+                return h if y is None else y
+            if st > 0:
+                self._check(st)
         tokens, D = x.shape if x.dim() == 2 else _bad("x", "need a matrix")
         F, t, d = w_gate.size(0) if w_gate.dim() == 2 else _bad("w_gate", "need a matrix"), x.dtype, self.device
         row, mid, win, wout = (tokens, D), (tokens, F), (F, D), (D, F)
@@ -634,6 +668,15 @@ class Context:
                                  dw_down=None, act=ACT_SILU):
         """Gradients of rtoss_gated_ffn_forward from dy and the kept gate and up, into those of dx, dw_gate, dw_up, dw_down
         that are given; h, dgate, dup [tokens, F] are workspaces (dgate may be gate and dup up)."""
+        if _F32 is None:
+            _types()
+        if _calls is not None:
+            st = _calls.gated_ffn_backward(self._h, self.device, x, w_gate, w_up, w_down, gate, up, dy, h, dgate, dup, dx, dw_gate, dw_up,
+                                           dw_down, act)
+            if st == 0:
+                return dx, dw_gate, dw_up, dw_down
+            if st > 0:
+                self._check(st)
         tokens, D = dy.shape if dy.dim() == 2 else _bad("dy", "need a matrix")
         F, t, d = w_down.size(1) if w_down.dim() == 2 else _bad("w_down", "need a matrix"), dy.dtype, self.device
         row, mid, win, wout = (tokens, D), (tokens, F), (F, D), (D, F)
@@ -654,6 +697,13 @@ class Context:
         share one).  Returns (z, n)."""
         if _F32 is None:
             _types()
+        if _calls is not None:
+            st = _calls.block_norm_forward(self._h, self.device, r, y, post, pre, post_weight, pre_weight, gate, tokens_per_gate, residual_scale,
+                                           eps, z, n)
+            if st == 0:
+                return z, n
+            if st > 0:
+                self._check(st)
         row = tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
         t, d, each = y.dtype, self.device, (D,)
         share = tokens_per_gate or max(tokens, 1)
@@ -680,6 +730,13 @@ class Context:
         may be None)."""
         if _F32 is None:
             _types()
+        if _calls is not None:
+            st = _calls.block_norm_backward(self._h, self.device, r, y, post, pre, post_weight, pre_weight, gate, tokens_per_gate, residual_scale,
+                                            eps, dz, dn, dr, dy, dpost_weight, dpre_weight, dgate, workspace)
+            if st == 0:
+                return dr, dy
+            if st > 0:
+                self._check(st)
         row = tokens, D = y.shape if y.dim() == 2 else _bad("y", "need a matrix")
         t, d, each = y.dtype, self.device, (D,)
         share = tokens_per_gate or max(tokens, 1)

@@ -1,0 +1,243 @@
+// The calls of the operators over tokens from Python (CPython extension module `_tok_calls`).
+//
+// A small call's time on the host is what it costs to look at its tensors: seven questions of 0.1 us each to a tensor from
+// Python, a few loads here.  Each function checks its operands and makes the library's call on the current stream.  Returned is
+// the library's status, or -1 when an operand is not what the call takes: binding.py then asks the same questions in Python
+// and raises the error that says which.  Nothing is kept between calls.
+#include <Python.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "rtoss.h"
+
+namespace {
+
+// The library's entry points (binding.py has loaded it).
+struct Entries {
+    decltype(&rtoss_quantize_rows) quantize_rows;
+    decltype(&rtoss_matmul_i8) matmul_i8;
+    decltype(&rtoss_gated_ffn_forward) ffn_forward;
+    decltype(&rtoss_gated_ffn_backward) ffn_backward;
+    decltype(&rtoss_block_norm_forward) norm_forward;
+    decltype(&rtoss_block_norm_backward) norm_backward;
+} g_entry;
+
+// One call's operands: the first that does not fit leaves `ok` false.
+struct Operands {
+    long device;
+    bool ok = true;
+
+    const at::Tensor* tensor(PyObject* o) {
+        if (!ok || !THPVariable_Check(o)) return ok = false, nullptr;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || t.get_device() != device) return ok = false, nullptr;
+        return &t;
+    }
+    // [rows, cols] of a matrix that decides a size
+    bool shape(PyObject* o, int64_t* rows, int64_t* cols, at::ScalarType* type) {
+        const at::Tensor* t = tensor(o);
+        if (!t || t->dim() != 2) return ok = false;
+        *rows = t->size(0), *cols = t->size(1), *type = t->scalar_type();
+        return *cols <= 0x7FFFFFFF || (ok = false);
+    }
+    rtoss_rows matrix(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type) {
+        rtoss_rows r = {nullptr, 0};
+        if (o == Py_None) return r;
+        const at::Tensor* t = tensor(o);
+        if (!t || t->scalar_type() != type || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (cols > 1 && t->stride(1) != 1) ||
+            (rows > 1 && t->stride(0) < cols)) {
+            ok = false;
+            return r;
+        }
+        r.dev = t->data_ptr();
+        r.row_stride = rows > 1 ? t->stride(0) : (cols + 15) / 16 * 16;   // (one row: no second one)
+        return r;
+    }
+    float* vector(PyObject* o, int64_t n) {
+        if (o == Py_None) return nullptr;
+        const at::Tensor* t = tensor(o);
+        if (!t || t->scalar_type() != at::kFloat || t->dim() != 1 || t->size(0) != n || !t->is_contiguous()) return ok = false, nullptr;
+        return static_cast<float*>(t->data_ptr());
+    }
+    rtoss_dtype dtype(at::ScalarType t) {
+        if (t == at::kFloat) return RTOSS_F32;
+        if (t == at::kBFloat16) return RTOSS_BF16;
+        if (t == at::kHalf) return RTOSS_F16;
+        ok = false;
+        return RTOSS_F32;
+    }
+    long number(PyObject* o) {
+        const long v = PyLong_AsLong(o);
+        if (v == -1 && PyErr_Occurred()) PyErr_Clear(), ok = false;
+        return v;
+    }
+    double real(PyObject* o) {
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) PyErr_Clear(), ok = false;
+        return v;
+    }
+};
+
+rtoss_ctx* context(PyObject* o) {
+    if (o == Py_None) return nullptr;
+    void* p = PyLong_AsVoidPtr(o);
+    if (!p && PyErr_Occurred()) PyErr_Clear();
+    return static_cast<rtoss_ctx*>(p);
+}
+
+// f(operands): fills in and returns a call of (context, stream); no C++ exception leaves.
+template <typename F>
+PyObject* guarded(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F&& f) {
+    long status = -1;
+    if (n == want) {
+        try {
+            Operands op;
+            op.device = PyLong_AsLong(a[1]);
+            if (PyErr_Occurred()) PyErr_Clear(), op.ok = false;
+            status = f(op, context(a[0]), a + 2);
+        } catch (...) {
+            status = -1;
+        }
+    }
+    return PyLong_FromLong(status);
+}
+template <typename Call>
+long on_stream(const Operands& op, Call&& call) {
+    if (!op.ok) return -1;
+    void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)op.device).stream();
+    long st;
+    Py_BEGIN_ALLOW_THREADS;
+    st = (long)call(stream);
+    Py_END_ALLOW_THREADS;
+    return st;
+}
+
+// (context, device, x, q, scale)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 5, [](Operands& op, rtoss_ctx* ctx, PyObject* const* o) {
+        int64_t rows, cols;
+        at::ScalarType t;
+        if (!op.shape(o[0], &rows, &cols, &t)) return -1l;
+        const rtoss_dtype dt = op.dtype(t);
+        const rtoss_rows x = op.matrix(o[0], rows, cols, t), q = op.matrix(o[1], rows, cols, at::kChar);
+        float* scale = op.vector(o[2], rows);
+        return on_stream(op, [&](void* s) {
+            return g_entry.quantize_rows(ctx, x.dev, dt, rows, (int)cols, x.row_stride, static_cast<int8_t*>(q.dev), q.row_stride, scale, s);
+        });
+    });
+}
+
+// (context, device, x, x_scale, w, w_scale, y, act, bias, residual, residual_after_act)
+PyObject* matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 11, [](Operands& op, rtoss_ctx* ctx, PyObject* const* o) {
+        int64_t tokens, K, N, k, ytok, yn;
+        at::ScalarType t, ty;
+        if (!op.shape(o[0], &tokens, &K, &t) || !op.shape(o[2], &N, &k, &t) || !op.shape(o[4], &ytok, &yn, &ty) || N > 0x7FFFFFFF) return -1l;
+        rtoss_i8_product p = {};
+        p.tokens = tokens, p.K = (int)K, p.N = (int)N;
+        p.x = op.matrix(o[0], tokens, K, at::kChar), p.w = op.matrix(o[2], N, K, at::kChar);
+        p.y = op.matrix(o[4], tokens, N, ty), p.residual = op.matrix(o[7], tokens, N, ty);
+        p.x_scale_dev = op.vector(o[1], tokens), p.w_scale_dev = op.vector(o[3], N), p.bias_dev = op.vector(o[6], N);
+        p.y_dtype = op.dtype(ty), p.act = (rtoss_act)op.number(o[5]), p.residual_after_act = (int)op.number(o[8]);
+        return on_stream(op, [&](void* s) { return g_entry.matmul_i8(ctx, &p, s); });
+    });
+}
+
+// (context, device, x, w_gate, w_up, w_down, h, y, gate, up, act)
+PyObject* gated_ffn_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 11, [](Operands& op, rtoss_ctx* ctx, PyObject* const* o) {
+        int64_t T, D, F, d;
+        at::ScalarType t, tw;
+        if (!op.shape(o[0], &T, &D, &t) || !op.shape(o[1], &F, &d, &tw) || F > 0x7FFFFFFF) return -1l;
+        rtoss_ffn f = {};
+        f.tokens = T, f.D = (int)D, f.F = (int)F, f.dtype = op.dtype(t), f.act = (rtoss_act)op.number(o[8]);
+        f.x = op.matrix(o[0], T, D, t), f.w_gate = op.matrix(o[1], F, D, t), f.w_up = op.matrix(o[2], F, D, t), f.w_down = op.matrix(o[3], D, F, t);
+        f.h = op.matrix(o[4], T, F, t), f.y = op.matrix(o[5], T, D, t), f.gate = op.matrix(o[6], T, F, t), f.up = op.matrix(o[7], T, F, t);
+        return on_stream(op, [&](void* s) { return g_entry.ffn_forward(ctx, &f, s); });
+    });
+}
+
+// (context, device, x, w_gate, w_up, w_down, gate, up, dy, h, dgate, dup, dx, dw_gate, dw_up, dw_down, act)
+PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 17, [](Operands& op, rtoss_ctx* ctx, PyObject* const* o) {
+        int64_t T, D, F, d;
+        at::ScalarType t, tw;
+        if (!op.shape(o[6], &T, &D, &t) || !op.shape(o[3], &d, &F, &tw)) return -1l;
+        rtoss_ffn f = {};
+        f.tokens = T, f.D = (int)D, f.F = (int)F, f.dtype = op.dtype(t), f.act = (rtoss_act)op.number(o[14]);
+        f.x = op.matrix(o[0], T, D, t), f.w_gate = op.matrix(o[1], F, D, t), f.w_up = op.matrix(o[2], F, D, t), f.w_down = op.matrix(o[3], D, F, t);
+        f.gate = op.matrix(o[4], T, F, t), f.up = op.matrix(o[5], T, F, t), f.dy = op.matrix(o[6], T, D, t), f.h = op.matrix(o[7], T, F, t);
+        f.dgate = op.matrix(o[8], T, F, t), f.dup = op.matrix(o[9], T, F, t), f.dx = op.matrix(o[10], T, D, t);
+        f.dw_gate = op.matrix(o[11], F, D, t), f.dw_up = op.matrix(o[12], F, D, t), f.dw_down = op.matrix(o[13], D, F, t);
+        return on_stream(op, [&](void* s) { return g_entry.ffn_backward(ctx, &f, s); });
+    });
+}
+
+// What both passes of the norms begin with, from o[0]: r, y, post, pre, post_weight, pre_weight, gate, tokens_per_gate,
+// residual_scale, eps.  -> rows that the gate has
+bool norm_operands(Operands& op, PyObject* const* o, rtoss_block_norm* b, at::ScalarType* t, int64_t* gates) {
+    int64_t T, D;
+    if (!op.shape(o[1], &T, &D, t)) return false;
+    const long share = op.number(o[7]);
+    b->tokens = T, b->D = (int)D, b->dtype = op.dtype(*t), b->post = (rtoss_norm)op.number(o[2]), b->pre = (rtoss_norm)op.number(o[3]);
+    b->residual_scale = (float)op.real(o[8]), b->eps = (float)op.real(o[9]);
+    b->tokens_per_gate = share ? share : T > 1 ? T : 1;
+    if (b->tokens_per_gate < 0) return op.ok = false;
+    *gates = T / b->tokens_per_gate > 1 ? T / b->tokens_per_gate : 1;
+    b->post_weight_dev = op.vector(o[4], D), b->pre_weight_dev = op.vector(o[5], D);
+    b->r = op.matrix(o[0], T, D, *t), b->y = op.matrix(o[1], T, D, *t), b->gate = op.matrix(o[6], *gates, D, *t);
+    return op.ok;
+}
+
+// (context, device, <norm_operands>, z, n)
+PyObject* block_norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 14, [](Operands& op, rtoss_ctx* ctx, PyObject* const* o) {
+        rtoss_block_norm b = {};
+        at::ScalarType t;
+        int64_t gates;
+        if (!norm_operands(op, o, &b, &t, &gates)) return -1l;
+        b.z = op.matrix(o[10], b.tokens, b.D, t), b.n = op.matrix(o[11], b.tokens, b.D, t);
+        return on_stream(op, [&](void* s) { return g_entry.norm_forward(ctx, &b, s); });
+    });
+}
+
+// (context, device, <norm_operands>, dz, dn, dr, dy, dpost_weight, dpre_weight, dgate, workspace)
+PyObject* block_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 20, [](Operands& op, rtoss_ctx* ctx, PyObject* const* o) {
+        rtoss_block_norm b = {};
+        at::ScalarType t;
+        int64_t gates;
+        if (!norm_operands(op, o, &b, &t, &gates)) return -1l;
+        b.dz = op.matrix(o[10], b.tokens, b.D, t), b.dn = op.matrix(o[11], b.tokens, b.D, t);
+        b.dr = op.matrix(o[12], b.tokens, b.D, t), b.dy = op.matrix(o[13], b.tokens, b.D, t);
+        b.dpost_weight_dev = op.vector(o[14], b.D), b.dpre_weight_dev = op.vector(o[15], b.D), b.dgate = op.matrix(o[16], gates, b.D, t);
+        if (o[17] != Py_None) {
+            const at::Tensor* w = op.tensor(o[17]);
+            if (!w) return -1l;
+            b.workspace_floats = w->numel();
+            b.workspace_dev = op.vector(o[17], w->numel());
+        }
+        return on_stream(op, [&](void* s) { return g_entry.norm_backward(ctx, &b, s); });
+    });
+}
+
+// entries(six addresses in the order of Entries)
+PyObject* entries(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void* p[6];
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "six addresses");
+    for (int i = 0; i < 6; ++i)
+        if (!(p[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "null address");
+    g_entry = {reinterpret_cast<decltype(g_entry.quantize_rows)>(p[0]), reinterpret_cast<decltype(g_entry.matmul_i8)>(p[1]),
+               reinterpret_cast<decltype(g_entry.ffn_forward)>(p[2]),   reinterpret_cast<decltype(g_entry.ffn_backward)>(p[3]),
+               reinterpret_cast<decltype(g_entry.norm_forward)>(p[4]),  reinterpret_cast<decltype(g_entry.norm_backward)>(p[5])};
+    Py_RETURN_NONE;
+}
+
+#define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+PyMethodDef g_methods[] = {CALL(entries),           CALL(quantize_rows),      CALL(matmul_i8), CALL(gated_ffn_forward), CALL(gated_ffn_backward),
+                           CALL(block_norm_forward), CALL(block_norm_backward), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tok_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__tok_calls() { return PyModule_Create(&g_module); }
