@@ -12,9 +12,9 @@
 // tokens (the gradients of weights and gates) end as one row per block in the workspace and are added in the blocks' order by
 // a second launch: no atomics, the same bits every time.  All arithmetic is fp32; squares are summed after the mean is
 // subtracted, not as a difference of moments.
-// Measured (bf16, cold): 16384 x 2048 forward 45.4 us, 5.9 TB/s; 8192 x 2048 forward 29.9, backward 55 (3.7 TB/s) and the sums over
-// tokens 8.5.  The backward pass is bound by its chain: a row's four sums over the block follow one another, with three rows
-// at a time on an SM.
+// Measured (bf16, cold): 16384 x 2048 forward 45.4 us, 5.9 TB/s; 8192 x 2048 forward 29.9, backward with the join of its sums over
+// tokens 46.9 (4.3 TB/s), which is bound by its instructions and its chain: a row's four sums over the block follow one another,
+// with four rows at a time on an SM.
 #include <atomic>
 
 #include "tok_internal.h"
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, false>()) norm_
 // gradient needs (they only lack the root, a factor); the two sums of the gradient of y's norm.
 // The gate and the weight of y's norm only ever come as their product, and the sums for both are one, A = sum of dz * yhat over
 // the rows that share a gate: dgate = weight * A, and dpost_weight gets gate * A.  So a thread holds four values for each of
-// its columns instead of six, and three blocks of 256 threads fit an SM.
+// its columns instead of six, and four blocks of 128 threads with two pieces each fit an SM.
 template <typename T, bool VEC, int G, int P>
 __global__ void __launch_bounds__(block_of<G>(), blocks_of<G, P, true>()) norm_backward_kernel(const NormArgs a) {
     NORM_UNIT(4, a.y, a.r, a.dz, a.dn);
@@ -801,7 +801,9 @@ __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArg
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
-// How rows are dealt out: threads of a unit by the row's length, units by what the device holds at once.
+// How rows are dealt out: threads of a unit by the row's length, units by what the device holds at once.  Backward, rows of more than
+// 1024 values give a thread two pieces: a third of the instructions were the sums over the block, which half the warps then share
+// (8192 x 2048 with their join: 52.8 -> 46.9 us; 16384 x 1024, where few threads are left, 48.1 -> 51.9).
 struct Plan {
     int G, P, threads, blocks, per_unit;   // threads: of a block; blocks: of an SM; per_unit: rows of a unit
     int parts, per_part;                   // blocks, each with a row of partial sums; rows of one
@@ -810,7 +812,7 @@ struct Plan {
 Plan plan_of(int64_t rows, int D, int sms, bool backward) {
     Plan p;
     const int pieces = (D + 7) / 8;
-    p.P = D <= (backward ? 2048 : 4096) ? 1 : D <= 8192 ? 2 : 0;
+    p.P = D <= (backward ? 1024 : 4096) ? 1 : D <= 8192 ? 2 : 0;
     const int each = p.P ? (pieces + p.P - 1) / p.P : 0;   // pieces of a thread's first round
     p.G = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : each <= 128 ? 128 : each <= 256 ? 256 : 512;
     if (p.P == 0) p.G = p.threads = kLongThreads, p.blocks = backward ? 1 : 2;
@@ -855,9 +857,10 @@ int launch_as(const rtoss_ctx* ctx, const Plan& p, NormArgs& a, cudaStream_t s) 
     if (p.G == 8) return launch_one<T, VEC, 8, 1, BACKWARD>(ctx, p, a, s);
     if (p.G == 16) return launch_one<T, VEC, 16, 1, BACKWARD>(ctx, p, a, s);
     if (p.G == 32) return launch_one<T, VEC, 32, 1, BACKWARD>(ctx, p, a, s);
-    if (p.G == 128) return launch_one<T, VEC, 128, 1, BACKWARD>(ctx, p, a, s);
+    if (p.G == 128 && p.P == 1) return launch_one<T, VEC, 128, 1, BACKWARD>(ctx, p, a, s);
     if (p.G == 256 && p.P == 1) return launch_one<T, VEC, 256, 1, BACKWARD>(ctx, p, a, s);
     if constexpr (BACKWARD) {
+        if (p.G == 128) return launch_one<T, VEC, 128, 2, BACKWARD>(ctx, p, a, s);
         if (p.G == 256) return launch_one<T, VEC, 256, 2, BACKWARD>(ctx, p, a, s);
     } else {
         if (p.P == 1) return launch_one<T, VEC, 512, 1, BACKWARD>(ctx, p, a, s);
