@@ -13,7 +13,7 @@
 // a second launch: no atomics, the same bits every time.  All arithmetic is fp32; squares are summed after the mean is
 // subtracted, not as a difference of moments.
 // Measured (bf16, cold): 16384 x 2048 forward 45.4 us, 5.9 TB/s; 8192 x 2048 forward 29.9, backward with the join of its sums over
-// tokens 46.9 (4.3 TB/s), which is bound by its instructions and its chain: a row's four sums over the block follow one another,
+// tokens 43.1 (4.7 TB/s), which is bound by its instructions and its chain: a row's four sums over the block follow one another,
 // with four rows at a time on an SM.
 #include <atomic>
 
@@ -749,13 +749,15 @@ struct JoinArgs {
     int D, parts, per_part, S, by_gate;   // parts: blocks that left sums; per_part: rows of one
 };
 
-// 32 threads with four columns each a block, 32 runs of partial sums side by side, joined in their order.
-constexpr int kJoinRuns = 32;
+// 32 columns a block (8 threads of four), 128 runs of partial sums side by side, joined in their order.  (With 128 columns and 32
+// runs the two weights' sums of 2048 columns kept 32 SMs busy: 10.2 us, now 9.4, and 8192 x 2048 without a gate 46.9 us with the backward pass, now 43.1.)
+constexpr int kJoinRuns = 128;
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArgs a) {
-    __shared__ float4 s[kJoinRuns][32];
+__global__ void __launch_bounds__(kJoinRuns * 8) norm_join_kernel(const JoinArgs a) {
+    __shared__ float4 s[kJoinRuns][8];
+    __shared__ float t[32][32];
     rtoss_dev::pdl_enter();
-    const int col = (int)blockIdx.x * 128 + ((int)threadIdx.x & 31) * 4, run = (int)threadIdx.x >> 5, what = (int)blockIdx.y;
+    const int col = (int)blockIdx.x * 32 + ((int)threadIdx.x & 7) * 4, run = (int)threadIdx.x >> 3, what = (int)blockIdx.y;
     const float* p = what == 0 ? a.p_post : a.p_pre;
     int first = 0, last = a.parts;   // rows that hold a share
     long long pitch = a.D;
@@ -786,18 +788,21 @@ __global__ void __launch_bounds__(kJoinRuns * 32) norm_join_kernel(const JoinArg
             else add(make_float4(at[0], col + 1 < a.D ? at[1] : 0.f, col + 2 < a.D ? at[2] : 0.f, col + 3 < a.D ? at[3] : 0.f));
         }
     }
-    s[run][threadIdx.x & 31] = sum;
+    s[run][threadIdx.x & 7] = sum;
     __syncthreads();
-    if (run < 4) {   // a column a thread
-        const int c = (int)threadIdx.x, at = (int)blockIdx.x * 128 + c;
-        float t = 0.f;
+    const int c = (int)threadIdx.x & 31, w = (int)threadIdx.x >> 5, at = (int)blockIdx.x * 32 + c;   // a column, four runs
+    float part = 0.f;
 #pragma unroll
-        for (int k = 0; k < kJoinRuns; ++k) t += reinterpret_cast<const float*>(s[k])[c];
-        if (at >= a.D) return;
-        if (what == 0) a.dpost[at] = t;
-        else if (what == 1) a.dpre[at] = t;
-        else reinterpret_cast<T*>(a.dgate)[row0 / a.S * a.dgate_ld + at] = from_f32<T>(t);
-    }
+    for (int k = 0; k < 4; ++k) part += reinterpret_cast<const float*>(s[4 * w + k])[c];
+    t[w][c] = part;
+    __syncthreads();
+    if (w > 0 || at >= a.D) return;
+    part = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) part += t[k][c];
+    if (what == 0) a.dpost[at] = part;
+    else if (what == 1) a.dpre[at] = part;
+    else reinterpret_cast<T*>(a.dgate)[row0 / a.S * a.dgate_ld + at] = from_f32<T>(part);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
@@ -939,9 +944,9 @@ int backward(const rtoss_ctx* ctx, const rtoss_block_norm* b, const Plan& p, cud
     if (!a.p_post && !a.p_pre && !join_gates) return 0;
     const int gates = (int)(b->tokens / a.S), by_gate = gates < p.parts;
     JoinArgs j = {a.p_post, a.p_pre, a.p_gate, b->dpost_weight_dev, b->dpre_weight_dev, a.dgate, a.dgate_ld, b->D, p.parts, p.per_part, a.S, by_gate};
-    const dim3 grid((unsigned)((b->D + 127) / 128), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.parts - 1)));
-    return b->D % 4 == 0 ? (int)rtoss_dev::launch_pdl(norm_join_kernel<T, true>, grid, dim3(kJoinRuns * 32), 0, s, j)
-                         : (int)rtoss_dev::launch_pdl(norm_join_kernel<T, false>, grid, dim3(kJoinRuns * 32), 0, s, j);
+    const dim3 grid((unsigned)((b->D + 31) / 32), (unsigned)(2 + (!join_gates ? 0 : by_gate ? gates : p.parts - 1)));
+    return b->D % 4 == 0 ? (int)rtoss_dev::launch_pdl(norm_join_kernel<T, true>, grid, dim3(kJoinRuns * 8), 0, s, j)
+                         : (int)rtoss_dev::launch_pdl(norm_join_kernel<T, false>, grid, dim3(kJoinRuns * 8), 0, s, j);
 }
 
 }  // namespace
