@@ -417,8 +417,11 @@ def _types():
     global _F32, _I8, _calls
     import torch
     from . import _build
-    if os.path.exists(_build.CALLS) and os.path.exists(_build.CALLS + ".stamp") and \
-            open(_build.CALLS + ".stamp").read().strip() == _build.calls_fingerprint():
+    try:
+        built = open(_build.CALLS + ".stamp").read().strip() == _build.calls_fingerprint()
+    except OSError:         # not built, or a package without its sources
+        built = False
+    if built:
         import importlib.util
         spec = importlib.util.spec_from_file_location("_tok_calls", _build.CALLS)
         calls = importlib.util.module_from_spec(spec)
