@@ -109,3 +109,65 @@ def test_on_the_current_stream():
         ctx().rtoss_quantize_rows(**args)
     side.synchronize()
     assert bool((args["q"] == 127).all())
+
+
+def test_threads_on_streams_of_their_own():
+    """Four threads, one context: each calls on its own stream with its own operands, over and over."""
+    import threading
+    sets = [operands() for _ in range(4)]
+    for f, args, _ in sets[0].values():
+        f(**args)
+    torch.cuda.synchronize()
+    want = {n: [sets[0][n][1][k].clone() for k in sets[0][n][2]] for n in NAMES}
+    errors = []
+
+    def work(mine):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    for n in NAMES:
+                        mine[n][0](**mine[n][1])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:   # (told below)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(m,)) for m in sets]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for mine in sets:
+        for n in NAMES:
+            for k, w in zip(mine[n][2], want[n]):
+                assert torch.equal(mine[n][1][k], w), (n, k)
+
+
+FIRST_CALLS = """
+import sys, torch
+sys.path[:0] = [%r, %r]
+import test_gpu_tok_calls as t
+sets = t.operands()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    for f, args, _ in sets.values():
+        f(**args)
+g.replay()
+torch.cuda.synchronize()
+got = {n: [sets[n][1][k].clone() for k in sets[n][2]] for n in t.NAMES}
+for f, args, _ in sets.values():
+    f(**args)
+torch.cuda.synchronize()
+assert all(torch.equal(a, sets[n][1][k]) for n in t.NAMES for a, k in zip(got[n], sets[n][2]))
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS % (here, os.path.dirname(here))], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
